@@ -299,6 +299,183 @@ tandem_status tandem_grpo_loss_noalloc(const tandem_grpo_cfg* cfg, const float* 
                                        float* advantages, float* grad, float* loss, int32_t* n_masked,
                                        void* stream);
 
+/* ------------------------------------------------------------------------
+ * The senior's update: what leads from the gradient of tandem_grpo_loss back
+ * to the weights of the next rollout (Algorithm 1's update half; Section 3.4).
+ * Handle-free like the loss: each call reads and writes caller-owned device
+ * memory, runs asynchronously on the given stream (hipStream_t as void*, NULL
+ * = the null stream of the current device; another stream's device is made
+ * current for the call), allocates nothing and may be captured into a HIP
+ * graph.  Workspaces are sized by the matching *_workspace_size call, 256-byte
+ * aligned, need no initialisation, and must not be shared by calls that may
+ * overlap (captured graphs that may run together included).  Results do not
+ * depend on the order in which the device runs its work.  Errors are reported
+ * through tandem_last_error(NULL); a call that fails before its first launch
+ * has written nothing.
+ * ------------------------------------------------------------------------ */
+
+/* Log-probs of the emitted tokens from the logits of a forward pass, and the
+ * divergence from a frozen reference model (the paper's KL-regularisation
+ * ablation: the reference is the junior).  Per row r, with
+ *   s_v = (z_v + eos_bias [v = eos_id]) / T         (the rollout's scores),
+ *   s'_v = (z'_v + eos_bias_ref [v = eos_id]) / T   (the reference's):
+ *   lse[r]      = log sum_v e^s_v
+ *   logp[r]     = s_y - lse[r],  y = tokens[r]
+ *   lse_diff[r] = lse[r] - log sum_v e^s'_v
+ *   kl[r]       = sum_v p_v (s_v - s'_v) - lse_diff[r] = KL(p || q),
+ * p = softmax(s), q = softmax(s'); a score of -inf has p_v = 0 and adds
+ * nothing, whatever the reference says there.
+ * A row whose token lies outside [0, vocab) (padding: -1) is left out: its
+ * outputs are 0, its gradient row is 0 and its logits are not read.  A row
+ * with a NaN or +inf logit has NaN outputs; one with nothing but -inf has an lse
+ * of -inf and NaN logp and kl. */
+typedef struct {
+  int32_t rows;                    /* R >= 0 */
+  int32_t vocab;                   /* V >= 1 */
+  int32_t dtype;                   /* of logits, reference logits and gradient: TANDEM_BF16 or TANDEM_F32 */
+  int32_t eos_id;                  /* < 0: no bias */
+  int64_t logits_stride;           /* elements from one row to the next, >= V */
+  int64_t ref_stride;              /* likewise; ignored without a reference */
+  int64_t grad_stride;             /* likewise, of the gradient; ignored by the forward pass */
+  float temperature;               /* T > 0, with a finite reciprocal */
+  float eos_bias, eos_bias_ref;
+} tandem_logprob_cfg;
+
+tandem_status tandem_logprob_workspace_size(const tandem_logprob_cfg* cfg, size_t* bytes);
+
+/* logits [R][V]; logits_ref [R][V] or NULL (no reference: kl and lse_diff
+ * must be NULL too, otherwise both are required); tokens int32 [R]; logp, lse,
+ * kl, lse_diff float [R] out. */
+tandem_status tandem_token_logprob(const tandem_logprob_cfg* cfg, const void* logits, const void* logits_ref,
+                                   const int32_t* tokens, float* logp, float* lse, float* kl, float* lse_diff,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+
+/* grad[r][v] = d/dz_v of sum_r (g_logp[r] logp[r] + g_kl[r] kl[r])
+ *            = (g_logp ([v = y] - p_v) + g_kl p_v (s_v - s'_v - lse_diff - kl)) / T.
+ * logits, logits_ref and tokens as in the forward pass, lse, kl and lse_diff
+ * its outputs; g_logp float [R]; g_kl float [R] or NULL (no KL term: then
+ * logits_ref, kl and lse_diff are not read and may be NULL).  grad [R][V] in
+ * the logits' dtype, every entry written; it may be the logits array itself
+ * (same pointer and stride), not overlap it otherwise.  A row whose g_logp and
+ * g_kl are both 0 gets a gradient of 0 and is not read. */
+tandem_status tandem_token_logprob_backward(const tandem_logprob_cfg* cfg, const void* logits,
+                                            const void* logits_ref, const int32_t* tokens, const float* lse,
+                                            const float* kl, const float* lse_diff, const float* g_logp,
+                                            const float* g_kl, void* grad, void* stream);
+
+/* Per-head RMSNorm of queries and keys and the rotary embedding, out of the
+ * packed QKV projection: what tandem_prefill does to a prompt row before its
+ * cache store, over rows of a training batch.  A row of qkv is n_q query
+ * heads, n_kv key heads and n_kv value heads of head_dim elements.  For a
+ * query or key head x at position t:
+ *   n = x r g,  r = 1 / sqrt(mean(x^2) + eps)       (gain NULL: n = x)
+ *   y_i = n_i cos a_i - n_{i+h} sin a_i,  y_{i+h} = n_{i+h} cos a_i + n_i sin a_i,
+ *   a_i = t theta^(-2i / head_dim), i < h = head_dim / 2,
+ * the angle reduced in 64 bits.  Positions are any int32.  Value heads are not
+ * touched.  Arrays are 16-byte aligned and strides multiples of 16 bytes. */
+typedef struct {
+  int32_t rows;                    /* N >= 0 */
+  int32_t n_q_heads, n_kv_heads;   /* >= 1 each, n_q % n_kv == 0 */
+  int32_t head_dim;                /* 32, 64 or 128 */
+  int32_t dtype;                   /* of qkv, q, k and their gradients */
+  float rope_theta, rms_eps;
+  int64_t qkv_stride;              /* elements between rows of qkv (and of dqkv) */
+  int64_t q_stride, k_stride;      /* elements between rows of q and k (of dq and dk) */
+} tandem_qk_cfg;
+
+tandem_status tandem_qk_workspace_size(const tandem_qk_cfg* cfg, size_t* bytes);
+
+/* q_gain, k_gain float [head_dim], both NULL for models without q/k norms;
+ * positions int32 [N]; q [N][n_q][hd], k [N][n_kv][hd] out. */
+tandem_status tandem_qk_norm_rope(const tandem_qk_cfg* cfg, const void* qkv, const float* q_gain,
+                                  const float* k_gain, const int32_t* positions, void* q, void* k, void* stream);
+
+/* dq and dk are the gradients of q and k.  dqkv receives the query and key
+ * columns' gradients (its value columns are left as they are); dq_gain and
+ * dk_gain float [head_dim] the gains' gradients summed over rows and heads
+ * (both NULL without gains).  The workspace may be NULL without gains. */
+tandem_status tandem_qk_norm_rope_backward(const tandem_qk_cfg* cfg, const void* qkv, const float* q_gain,
+                                           const float* k_gain, const int32_t* positions, const void* dq,
+                                           const void* dk, void* dqkv, float* dq_gain, float* dk_gain,
+                                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* Causal grouped-query attention over packed sequences, with the statistics
+ * its gradient needs.  Rows offsets[s] .. offsets[s+1]-1 of q, k, v are
+ * sequence s; row i of a sequence attends its rows j <= i:
+ *   lse[h][i] = log sum_j e^{scale q_i . k_j},  out_i = sum_j e^{scale q_i . k_j - lse_i} v_j,
+ * query head h reading key head h / (n_q / n_kv).  offsets is a device array
+ * of n_seqs + 1 non-decreasing int32 in [0, N] (values outside are clamped, so
+ * no access leaves the arrays; empty sequences are allowed); rows before
+ * offsets[0] and from offsets[n_seqs] on belong to no sequence and their
+ * outputs are left as they are.  bf16 inputs: products on the matrix cores
+ * with float32 sums, probabilities rounded to bf16 for the value product.
+ * Values must be finite: a NaN or infinity in one row of v reaches other rows
+ * of the same sequence.
+ * Heads of a row are contiguous ([n][head_dim]); arrays are 16-byte aligned
+ * and strides multiples of 16 bytes, so q, k and v may be columns of one
+ * projection. */
+typedef struct {
+  int32_t rows;                    /* N >= 0, the rows of every array */
+  int32_t n_seqs;                  /* >= 0 */
+  int32_t n_q_heads, n_kv_heads;   /* n_q % n_kv == 0 */
+  int32_t head_dim;                /* 32, 64 or 128 */
+  int32_t dtype;                   /* TANDEM_BF16 or TANDEM_F32 */
+  float scale;                     /* finite, > 0; 1 / sqrt(head_dim) in the models here */
+  int64_t q_stride, k_stride, v_stride, out_stride;         /* elements between rows */
+  int64_t dout_stride, dq_stride, dk_stride, dv_stride;     /* ignored by the forward pass */
+} tandem_attention_cfg;
+
+/* Workspace of the backward pass (the forward pass needs none). */
+tandem_status tandem_attention_workspace_size(const tandem_attention_cfg* cfg, size_t* bytes);
+/* out [N][n_q][hd]; lse float [n_q][N]. */
+tandem_status tandem_attention(const tandem_attention_cfg* cfg, const void* q, const void* k, const void* v,
+                               const int32_t* offsets, void* out, float* lse, void* stream);
+/* dq, dk and dv (in dtype) for the gradient dout of out, from the forward
+ * pass's inputs and outputs; the probabilities are computed again.  A key
+ * head's gradient is the sum over the query heads that read it. */
+tandem_status tandem_attention_backward(const tandem_attention_cfg* cfg, const void* dout, const void* q,
+                                        const void* k, const void* v, const void* out, const float* lse,
+                                        const int32_t* offsets, void* dq, void* dk, void* dv, void* workspace,
+                                        size_t workspace_bytes, void* stream);
+
+/* One AdamW step over all tensors of a model.  With g the gradient, t the
+ * step's number (1 for the first), w the weight in float32 (its master copy,
+ * or the weight itself without one):
+ *   norm = sqrt(sum over all tensors of g^2);  c = min(1, max_norm / (norm + 1e-6))
+ *          (c = 1 and norm is not computed when max_norm = 0)
+ *   m = beta1 m + (1 - beta1) c g;   v = beta2 v + (1 - beta2) (c g)^2
+ *   w = w (1 - lr decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+ * States are float32; a bf16 weight is w rounded once.  m, v and master are
+ * arenas of arena_elems floats in which tensor i occupies
+ * [state_offset, state_offset + n), state_offset a multiple of 4; master NULL:
+ * no master copies.  tensors is a HOST array that is read during the call.
+ * Weights, gradients and arenas do not overlap. */
+typedef struct {
+  void* param;                     /* weights, updated in place */
+  const void* grad;
+  int64_t n;                       /* elements, >= 0 */
+  int64_t state_offset;            /* elements into the arenas, multiple of 4 */
+  double weight_decay;             /* finite, >= 0 */
+  int32_t param_dtype, grad_dtype; /* TANDEM_BF16 or TANDEM_F32 */
+} tandem_adamw_tensor;
+
+typedef struct {
+  double lr;                       /* finite */
+  double beta1, beta2;             /* in [0, 1) */
+  double eps;                      /* finite, > 0 as a float */
+  double max_norm;                 /* finite, >= 0; 0: no clipping */
+  int32_t step;                    /* t >= 1 */
+  int64_t arena_elems;             /* size of each arena */
+} tandem_adamw_cfg;
+
+/* Workspace of a step with clipping (0 bytes without). */
+tandem_status tandem_adamw_workspace_size(const tandem_adamw_cfg* cfg, const tandem_adamw_tensor* tensors,
+                                          int32_t n_tensors, size_t* bytes);
+/* norm float [1] out (required with clipping, else ignored): the norm before clipping. */
+tandem_status tandem_adamw(const tandem_adamw_cfg* cfg, const tandem_adamw_tensor* tensors, int32_t n_tensors,
+                           float* m, float* v, float* master, float* norm, void* workspace, size_t workspace_bytes,
+                           void* stream);
+
 /* The per-request sampler state of the reproducibility appendix (current
  * owner, span counter, step, position, finished), copied to HOST int32
  * arrays of n_seqs entries (any pointer may be NULL): owner (1 = senior),

@@ -59,10 +59,43 @@ class GrpoCfg(C.Structure):
                 ("clip_eps", C.c_float)]
 
 
+class LogprobCfg(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("vocab", C.c_int32), ("dtype", C.c_int32), ("eos_id", C.c_int32),
+                ("logits_stride", C.c_int64), ("ref_stride", C.c_int64), ("grad_stride", C.c_int64),
+                ("temperature", C.c_float), ("eos_bias", C.c_float), ("eos_bias_ref", C.c_float)]
+
+
+class QkCfg(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("dtype", C.c_int32), ("rope_theta", C.c_float), ("rms_eps", C.c_float),
+                ("qkv_stride", C.c_int64), ("q_stride", C.c_int64), ("k_stride", C.c_int64)]
+
+
+class AttentionCfg(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("n_seqs", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float),
+                ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64), ("out_stride", C.c_int64),
+                ("dout_stride", C.c_int64), ("dq_stride", C.c_int64), ("dk_stride", C.c_int64),
+                ("dv_stride", C.c_int64)]
+
+
+class AdamwTensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("n", C.c_int64), ("state_offset", C.c_int64),
+                ("weight_decay", C.c_double), ("param_dtype", C.c_int32), ("grad_dtype", C.c_int32)]
+
+
+class AdamwCfg(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("max_norm", C.c_double), ("step", C.c_int32), ("arena_elems", C.c_int64)]
+
+
 EXPORTS = ("tandem_workspace_size", "tandem_init", "tandem_prefill", "tandem_step",
            "tandem_step_forced", "tandem_score_step", "tandem_get_state", "tandem_timing_enable", "tandem_timing_read",
            "tandem_last_error", "tandem_status_string", "tandem_destroy", "tandem_grpo_workspace_size",
-           "tandem_grpo_loss", "tandem_grpo_loss_noalloc")
+           "tandem_grpo_loss", "tandem_grpo_loss_noalloc", "tandem_logprob_workspace_size", "tandem_token_logprob",
+           "tandem_token_logprob_backward", "tandem_qk_workspace_size", "tandem_qk_norm_rope",
+           "tandem_qk_norm_rope_backward", "tandem_attention_workspace_size", "tandem_attention",
+           "tandem_attention_backward", "tandem_adamw_workspace_size", "tandem_adamw")
 K_ATTENTION, K_GEMM, K_SAMPLE, K_OTHER = 0, 1, 2, 3
 TIMING_SERIAL = 1 << 8          # timing flag: run the two forwards one after the other
 TIMING_EAGER = 1 << 9           # timing flag: launch every kernel from the host (no step graph)
@@ -111,6 +144,20 @@ def _load():
     lib.tandem_grpo_loss.restype = st
     lib.tandem_grpo_loss_noalloc.argtypes = [C.POINTER(GrpoCfg), P, P, P, P, P, P, P, P, P, P]
     lib.tandem_grpo_loss_noalloc.restype = st
+    Z, Q = C.c_size_t, C.POINTER(C.c_size_t)
+    lib.tandem_logprob_workspace_size.argtypes = [C.POINTER(LogprobCfg), Q]
+    lib.tandem_token_logprob.argtypes = [C.POINTER(LogprobCfg)] + [P] * 8 + [Z, P]
+    lib.tandem_token_logprob_backward.argtypes = [C.POINTER(LogprobCfg)] + [P] * 10
+    lib.tandem_qk_workspace_size.argtypes = [C.POINTER(QkCfg), Q]
+    lib.tandem_qk_norm_rope.argtypes = [C.POINTER(QkCfg)] + [P] * 7
+    lib.tandem_qk_norm_rope_backward.argtypes = [C.POINTER(QkCfg)] + [P] * 10 + [Z, P]
+    lib.tandem_attention_workspace_size.argtypes = [C.POINTER(AttentionCfg), Q]
+    lib.tandem_attention.argtypes = [C.POINTER(AttentionCfg)] + [P] * 7
+    lib.tandem_attention_backward.argtypes = [C.POINTER(AttentionCfg)] + [P] * 11 + [Z, P]
+    lib.tandem_adamw_workspace_size.argtypes = [C.POINTER(AdamwCfg), C.POINTER(AdamwTensor), C.c_int32, Q]
+    lib.tandem_adamw.argtypes = [C.POINTER(AdamwCfg), C.POINTER(AdamwTensor), C.c_int32] + [P] * 5 + [Z, P]
+    for name in EXPORTS[15:]:
+        getattr(lib, name).restype = st
     return lib
 
 
@@ -209,3 +256,68 @@ def tandem_grpo_loss_noalloc(cfg: GrpoCfg, rewards: int, owner: int, length: int
                              advantages: int, grad, loss: int, n_masked: int, stream: int) -> None:
     check(lib.tandem_grpo_loss_noalloc(C.byref(cfg), rewards, owner, length, logp_old, logp_new, advantages,
                                        grad, loss, n_masked, stream))
+
+
+# ------------------------------------------------- the senior's update
+
+def tandem_logprob_workspace_size(cfg: LogprobCfg) -> int:
+    n = C.c_size_t()
+    check(lib.tandem_logprob_workspace_size(C.byref(cfg), C.byref(n)))
+    return n.value
+
+
+def tandem_token_logprob(cfg: LogprobCfg, logits: int, logits_ref, tokens: int, logp: int, lse: int, kl, lse_diff,
+                         workspace, workspace_bytes: int, stream: int) -> None:
+    check(lib.tandem_token_logprob(C.byref(cfg), logits, logits_ref, tokens, logp, lse, kl, lse_diff, workspace,
+                                   workspace_bytes, stream))
+
+
+def tandem_token_logprob_backward(cfg: LogprobCfg, logits: int, logits_ref, tokens: int, lse: int, kl, lse_diff,
+                                  g_logp: int, g_kl, grad: int, stream: int) -> None:
+    check(lib.tandem_token_logprob_backward(C.byref(cfg), logits, logits_ref, tokens, lse, kl, lse_diff, g_logp, g_kl,
+                                            grad, stream))
+
+
+def tandem_qk_workspace_size(cfg: QkCfg) -> int:
+    n = C.c_size_t()
+    check(lib.tandem_qk_workspace_size(C.byref(cfg), C.byref(n)))
+    return n.value
+
+
+def tandem_qk_norm_rope(cfg: QkCfg, qkv: int, q_gain, k_gain, positions: int, q: int, k: int, stream: int) -> None:
+    check(lib.tandem_qk_norm_rope(C.byref(cfg), qkv, q_gain, k_gain, positions, q, k, stream))
+
+
+def tandem_qk_norm_rope_backward(cfg: QkCfg, qkv: int, q_gain, k_gain, positions: int, dq: int, dk: int, dqkv: int,
+                                 dq_gain, dk_gain, workspace, workspace_bytes: int, stream: int) -> None:
+    check(lib.tandem_qk_norm_rope_backward(C.byref(cfg), qkv, q_gain, k_gain, positions, dq, dk, dqkv, dq_gain,
+                                           dk_gain, workspace, workspace_bytes, stream))
+
+
+def tandem_attention_workspace_size(cfg: AttentionCfg) -> int:
+    n = C.c_size_t()
+    check(lib.tandem_attention_workspace_size(C.byref(cfg), C.byref(n)))
+    return n.value
+
+
+def tandem_attention(cfg: AttentionCfg, q: int, k: int, v: int, offsets: int, out: int, lse: int,
+                     stream: int) -> None:
+    check(lib.tandem_attention(C.byref(cfg), q, k, v, offsets, out, lse, stream))
+
+
+def tandem_attention_backward(cfg: AttentionCfg, dout: int, q: int, k: int, v: int, out: int, lse: int, offsets: int,
+                              dq: int, dk: int, dv: int, workspace: int, workspace_bytes: int, stream: int) -> None:
+    check(lib.tandem_attention_backward(C.byref(cfg), dout, q, k, v, out, lse, offsets, dq, dk, dv, workspace,
+                                        workspace_bytes, stream))
+
+
+def tandem_adamw_workspace_size(cfg: AdamwCfg, tensors, n_tensors: int) -> int:
+    """tensors: a ctypes array of AdamwTensor."""
+    n = C.c_size_t()
+    check(lib.tandem_adamw_workspace_size(C.byref(cfg), tensors, n_tensors, C.byref(n)))
+    return n.value
+
+
+def tandem_adamw(cfg: AdamwCfg, tensors, n_tensors: int, m: int, v: int, master, norm, workspace,
+                 workspace_bytes: int, stream: int) -> None:
+    check(lib.tandem_adamw(C.byref(cfg), tensors, n_tensors, m, v, master, norm, workspace, workspace_bytes, stream))

@@ -20,7 +20,8 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libtandem.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
-SOURCES = ["tandem.cpp", "k_gemm.hip", "k_stream.hip", "k_attn.hip", "k_misc.hip", "k_grpo.hip"]
+SOURCES = ["tandem.cpp", "k_gemm.hip", "k_stream.hip", "k_attn.hip", "k_misc.hip", "k_grpo.hip",
+           "update.cpp", "k_logprob.hip", "k_qk.hip", "k_flash.hip", "k_adamw.hip"]
 
 
 def hip_runtime_dir() -> str:

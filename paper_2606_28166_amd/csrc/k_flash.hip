@@ -1,0 +1,446 @@
+// k_flash.hip — causal grouped-query attention over packed sequences: the forward
+// pass with its log-sum-exps, and the backward pass, which computes the
+// probabilities again.
+//
+// Scores are formed with the 32 x 32 matrix instructions, on blocks of 32 queries by
+// 32 keys.  Their result layout puts one column in a lane (column = lane % 32) and 16
+// of the 32 rows in its registers (row = 8 (i / 4) + 4 (lane / 32) + i % 4 of
+// register i); that is, up to the order of the summed index, the layout in which the
+// next product takes its right operand.  So probabilities and their gradients go
+// from one product into the next in registers, and only the left operands, which the
+// waves of a workgroup share, pass through LDS: by rows (summed over the head
+// dimension) and transposed (summed over positions).
+//   forward   S^T = K Q^T, O^T += V^T P^T          a column is a query
+//   dQ        S^T, dP^T = V dO^T, dQ^T += K^T dS^T  a column is a query
+//   dK, dV    S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS   a column is a key
+// dQ and dK/dV are separate passes: each output is summed by one wave in a fixed
+// order (no atomics), for 7 products where one pass would take 5.
+// float32 models run the same code on the float32 matrix instructions.
+#include "common.h"
+#include "update.h"
+
+namespace tandem {
+namespace {
+
+typedef short s16x4_v __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4_v lds_s16x4_v;
+
+constexpr int kRows = 64;        // rows of a staged tile
+constexpr int kWaves = 4;        // waves of a workgroup
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ f32x16_t zero16() {
+  f32x16_t z;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) z[i] = 0.f;
+  return z;
+}
+// row of register i in a 32 x 32 result, h = lane / 32
+__device__ __forceinline__ int result_row(int i, int h) { return 8 * (i >> 2) + 4 * h + (i & 3); }
+
+// A tile of rows of HD elements in LDS, in 16-byte chunks that are permuted by row
+// so that both readers spread over the banks: eight consecutive rows' chunks c (rows
+// as left operand) and the 32-byte pieces of four consecutive rows (transposed).
+template <typename T, int HD> struct Ops;
+
+template <int HD> struct Ops<bf16_t, HD> {
+  static constexpr int CPR = HD / 8;                       // chunks per row
+  static constexpr int ROW = HD * 2;                       // bytes per row
+  struct Right { bf16x8_t b[HD / 16]; };                   // 32 columns, summed over the head dimension
+  struct Prob { bf16x8_t b[2]; };                          // 32 x 32, summed over its rows
+
+  __device__ __forceinline__ static int at(int row, int c) {
+    const int f = CPR >= 8 ? ((row & 3) << 1) | ((row >> 2) & 1) : (((row >> 1) & 1) << 1) | ((row >> 2) & 1);
+    return row * ROW + ((c ^ f) << 4);
+  }
+  // p: the column's row in memory
+  __device__ __forceinline__ static void load_right(Right& r, const bf16_t* p, int h) {
+#pragma unroll
+    for (int k = 0; k < HD / 16; ++k) r.b[k] = *reinterpret_cast<const bf16x8_t*>(p + 16 * k + 8 * h);
+  }
+  __device__ __forceinline__ static Prob pack(const float* p) {
+    Prob r;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) r.b[i >> 3][i & 7] = (__bf16)p[i];
+    return r;
+  }
+  // acc += tile rows r0 .. r0 + 31 by right
+  __device__ __forceinline__ static f32x16_t by_rows(f32x16_t acc, const char* tile, int r0, const Right& right,
+                                                     int lane) {
+#pragma unroll
+    for (int k = 0; k < HD / 16; ++k) {
+      const bf16x8_t a =
+          *reinterpret_cast<const bf16x8_t*>(tile + at(r0 + (lane & 31), 2 * k + (lane >> 5)));
+      acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, right.b[k], acc, 0, 0, 0);
+    }
+    return acc;
+  }
+  // acc[d / 32] += (tile rows r0 .. r0 + 31)^T by p
+  __device__ __forceinline__ static void transposed(f32x16_t* acc, const char* tile, int r0, const Prob& p,
+                                                    int lane) {
+    const int h = lane >> 5, g = (lane >> 4) & 1, i = lane & 15;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      const int row = r0 + 16 * kb + 4 * h + (i >> 2);
+#pragma unroll
+      for (int d = 0; d < HD / 32; ++d) {
+        const int c = 4 * d + 2 * g + ((i & 3) >> 1), b = (i & 1) * 8;
+        const s16x4_v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_v*)(tile + at(row, c) + b));
+        const s16x4_v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_v*)(tile + at(row + 8, c) + b));
+        typedef short s16x8_v __attribute__((ext_vector_type(8)));
+        const s16x8_v a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), p.b[kb], acc[d], 0, 0, 0);
+      }
+    }
+  }
+};
+
+template <int HD> struct Ops<float, HD> {
+  static constexpr int CPR = HD / 4;
+  static constexpr int ROW = HD * 4;
+  struct Right { float b[HD / 2]; };
+  struct Prob { float b[16]; };
+
+  __device__ __forceinline__ static int at(int row, int c) { return row * ROW + ((c ^ (row & 7)) << 4); }
+  __device__ __forceinline__ static void load_right(Right& r, const float* p, int h) {
+#pragma unroll
+    for (int k = 0; k < HD / 8; ++k) {
+      const f32x4_t v = *reinterpret_cast<const f32x4_t*>(p + h * (HD / 2) + 4 * k);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) r.b[4 * k + e] = v[e];
+    }
+  }
+  __device__ __forceinline__ static Prob pack(const float* p) {
+    Prob r;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) r.b[i] = p[i];
+    return r;
+  }
+  __device__ __forceinline__ static f32x16_t by_rows(f32x16_t acc, const char* tile, int r0, const Right& right,
+                                                     int lane) {
+#pragma unroll
+    for (int k = 0; k < HD / 8; ++k) {
+      const f32x4_t a =
+          *reinterpret_cast<const f32x4_t*>(tile + at(r0 + (lane & 31), (lane >> 5) * (HD / 8) + k));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], right.b[4 * k + e], acc, 0, 0, 0);
+    }
+    return acc;
+  }
+  __device__ __forceinline__ static void transposed(f32x16_t* acc, const char* tile, int r0, const Prob& p,
+                                                    int lane) {
+    const int h = lane >> 5, c = lane & 31;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int row = r0 + result_row(i, h);
+#pragma unroll
+      for (int d = 0; d < HD / 32; ++d) {
+        const float a = *reinterpret_cast<const float*>(tile + at(row, 8 * d + (c >> 2)) + (c & 3) * 4);
+        acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p.b[i], acc[d], 0, 0, 0);
+      }
+    }
+  }
+};
+
+// kRows rows from g (row stride ld elements) into a tile; rows at or past `valid` are zero.
+template <typename T, int HD>
+__device__ __forceinline__ void stage(char* tile, const T* g, int64_t ld, int valid) {
+  using O = Ops<T, HD>;
+  constexpr int EPC = 16 / sizeof(T);
+  for (int i = threadIdx.x; i < kRows * O::CPR; i += 64 * kWaves) {
+    const int row = i / O::CPR, c = i % O::CPR;
+    u32x4_t v = {0, 0, 0, 0};
+    if (row < valid) v = *reinterpret_cast<const u32x4_t*>(g + row * ld + c * EPC);
+    *reinterpret_cast<u32x4_t*>(tile + O::at(row, c)) = v;
+  }
+}
+
+// Columns of a 32 x 32 result block row back to memory: lane (column, h) writes, per 32
+// dimensions, four runs of four.
+__device__ __forceinline__ void store4(bf16_t* p, float a, float b, float c, float d) {
+  typedef __bf16 bf16x4_v __attribute__((ext_vector_type(4)));
+  *reinterpret_cast<bf16x4_v*>(p) = bf16x4_v{(__bf16)a, (__bf16)b, (__bf16)c, (__bf16)d};
+}
+__device__ __forceinline__ void store4(float* p, float a, float b, float c, float d) {
+  *reinterpret_cast<f32x4_t*>(p) = f32x4_t{a, b, c, d};
+}
+template <typename T, int HD>
+__device__ __forceinline__ void store_column(T* p, const f32x16_t* acc, float by, int h) {
+#pragma unroll
+  for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      store4(p + 32 * d + 8 * j + 4 * h, acc[d][4 * j] * by, acc[d][4 * j + 1] * by, acc[d][4 * j + 2] * by,
+             acc[d][4 * j + 3] * by);
+}
+
+// The tile of a workgroup: sequence s owns the slots from off[s] / per + s on, one per
+// `per` positions, which are enough for it; slots past its length are empty.
+struct Span {
+  int start, len, first;         // first row and length of the sequence; first position of the tile (>= len: none)
+};
+__device__ __forceinline__ Span find_span(const int32_t* offs, int n_seqs, int N, int slot, int per) {
+  const int lane = threadIdx.x & 63;
+  int s = -1;
+  for (int b = 0; b < n_seqs; b += kWave) {
+    const int i = b + lane;
+    const int o = i < n_seqs ? min(max(offs[i], 0), N) : 0;
+    s += __popcll(__ballot(i < n_seqs && o / per + i <= slot));
+  }
+  Span r = {0, 0, 0};
+  if (s < 0) return r;
+  s = __builtin_amdgcn_readfirstlane(s);
+  r.start = min(max(offs[s], 0), N);
+  r.len = min(max(offs[s + 1], r.start), N) - r.start;
+  r.first = (slot - (r.start / per + s)) * per;
+  return r;
+}
+
+// Query heads of a key head that share a workgroup (the rest of its waves take other
+// positions): the largest power of two that divides the group, up to the waves.
+__host__ __device__ inline int heads_together(int group) {
+  int n = 1;
+  while (2 * n <= kWaves && group % (2 * n) == 0) n *= 2;
+  return n;
+}
+
+template <typename T, int HD>
+__global__ __launch_bounds__(64 * kWaves) void flash_kernel(FlashArgs a, int slots) {
+  using O = Ops<T, HD>;
+  __shared__ __align__(16) char tk[kRows * O::ROW], tv[kRows * O::ROW];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5, col = lane & 31;
+  const int group = a.nq / a.nkv, together = heads_together(group), per = 32 * (kWaves / together);
+  const int kv = blockIdx.x % a.nkv, sub = blockIdx.x / a.nkv % (group / together);
+  // the last tiles of a sequence are its longest: they go first
+  const int slot = slots - 1 - blockIdx.x / a.nkv / (group / together);
+  const Span w = find_span(a.offs, a.n_seqs, a.N, slot, per);
+  if (w.first >= w.len) return;
+  const int head = kv * group + sub * together + wave % together;
+  const int q0 = w.first + 32 * (wave / together), qi = q0 + col;
+  const int64_t row = w.start + min(qi, w.len - 1);
+  typename O::Right q;
+  O::load_right(q, reinterpret_cast<const T*>(a.q) + row * a.ldq + head * HD, h);
+  const T* kb = reinterpret_cast<const T*>(a.k) + (int64_t)w.start * a.ldk + kv * HD;
+  const T* vb = reinterpret_cast<const T*>(a.v) + (int64_t)w.start * a.ldv + kv * HD;
+  const float s2 = a.scale * kLog2e;
+  float m = -INFINITY, l = 0.f;
+  f32x16_t o[HD / 32];
+#pragma unroll
+  for (int d = 0; d < HD / 32; ++d) o[d] = zero16();
+  const int end = min(w.len, w.first + per);               // keys that any row of the tile sees
+  for (int n0 = 0; n0 < end; n0 += kRows) {
+    __syncthreads();
+    stage<T, HD>(tk, kb + (int64_t)n0 * a.ldk, a.ldk, w.len - n0);
+    stage<T, HD>(tv, vb + (int64_t)n0 * a.ldv, a.ldv, w.len - n0);
+    __syncthreads();
+    if (n0 > q0 + 31) continue;
+    f32x16_t s[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) s[b] = O::by_rows(zero16(), tk, 32 * b, q, lane);
+    if (n0 + kRows - 1 > q0) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (n0 + 32 * b + result_row(i, h) > qi) s[b][i] = -INFINITY;
+    }
+    float mx = m;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
+    mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+    const float f = __builtin_amdgcn_exp2f((m - mx) * s2);
+    m = mx;
+    l *= f;
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d) o[d] *= f;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      float p[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        p[i] = __builtin_amdgcn_exp2f((s[b][i] - m) * s2);
+        l += p[i];
+      }
+      O::transposed(o, tv, 32 * b, O::pack(p), lane);
+    }
+  }
+  l += __shfl_xor(l, 32, kWave);
+  if (qi >= w.len) return;
+  store_column<T, HD>(reinterpret_cast<T*>(a.out) + row * a.ldo + head * HD, o, 1.f / l, h);
+  if (h == 0) a.lse[(int64_t)head * a.N + row] = m * a.scale + logf(l);
+}
+
+// delta[h][i] = dout_i . out_i, HD / 8 lanes per (row, head)
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void flash_delta_kernel(FlashArgs a) {
+  constexpr int LANES = HD / 8;
+  const int64_t item = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LANES;
+  const int c = threadIdx.x % LANES;
+  if (item >= (int64_t)a.N * a.nq) return;
+  const int64_t row = item / a.nq;
+  const int head = (int)(item % a.nq);
+  const T* o = reinterpret_cast<const T*>(a.out) + row * a.ldo + head * HD + 8 * c;
+  const T* g = reinterpret_cast<const T*>(a.dout) + row * a.lddo + head * HD + 8 * c;
+  float s = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s += ld(o + e) * ld(g + e);
+#pragma unroll
+  for (int x = LANES / 2; x > 0; x >>= 1) s += __shfl_xor(s, x, kWave);
+  if (c == 0) a.delta[(int64_t)head * a.N + row] = s;
+}
+
+template <typename T, int HD>
+__global__ __launch_bounds__(64 * kWaves) void flash_dq_kernel(FlashArgs a, int slots) {
+  using O = Ops<T, HD>;
+  __shared__ __align__(16) char tk[kRows * O::ROW], tv[kRows * O::ROW];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5, col = lane & 31;
+  const int group = a.nq / a.nkv, together = heads_together(group), per = 32 * (kWaves / together);
+  const int kv = blockIdx.x % a.nkv, sub = blockIdx.x / a.nkv % (group / together);
+  const int slot = slots - 1 - blockIdx.x / a.nkv / (group / together);
+  const Span w = find_span(a.offs, a.n_seqs, a.N, slot, per);
+  if (w.first >= w.len) return;
+  const int head = kv * group + sub * together + wave % together;
+  const int q0 = w.first + 32 * (wave / together), qi = q0 + col;
+  const int64_t row = w.start + min(qi, w.len - 1);
+  typename O::Right q, g;
+  O::load_right(q, reinterpret_cast<const T*>(a.q) + row * a.ldq + head * HD, h);
+  O::load_right(g, reinterpret_cast<const T*>(a.dout) + row * a.lddo + head * HD, h);
+  const float lse = a.lse[(int64_t)head * a.N + row] * kLog2e, delta = a.delta[(int64_t)head * a.N + row];
+  const T* kb = reinterpret_cast<const T*>(a.k) + (int64_t)w.start * a.ldk + kv * HD;
+  const T* vb = reinterpret_cast<const T*>(a.v) + (int64_t)w.start * a.ldv + kv * HD;
+  const float s2 = a.scale * kLog2e;
+  f32x16_t dq[HD / 32];
+#pragma unroll
+  for (int d = 0; d < HD / 32; ++d) dq[d] = zero16();
+  const int end = min(w.len, w.first + per);
+  for (int n0 = 0; n0 < end; n0 += kRows) {
+    __syncthreads();
+    stage<T, HD>(tk, kb + (int64_t)n0 * a.ldk, a.ldk, w.len - n0);
+    stage<T, HD>(tv, vb + (int64_t)n0 * a.ldv, a.ldv, w.len - n0);
+    __syncthreads();
+    if (n0 > q0 + 31) continue;
+    const bool edge = n0 + kRows - 1 > q0;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const f32x16_t s = O::by_rows(zero16(), tk, 32 * b, q, lane);
+      const f32x16_t dp = O::by_rows(zero16(), tv, 32 * b, g, lane);
+      float ds[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], s2, -lse));
+        ds[i] = p * (dp[i] - delta);
+        if (edge && n0 + 32 * b + result_row(i, h) > qi) ds[i] = 0.f;
+      }
+      O::transposed(dq, tk, 32 * b, O::pack(ds), lane);
+    }
+  }
+  if (qi >= w.len) return;
+  store_column<T, HD>(reinterpret_cast<T*>(a.dq) + row * a.lddq + head * HD, dq, a.scale, h);
+}
+
+template <typename T, int HD>
+__global__ __launch_bounds__(64 * kWaves) void flash_dkv_kernel(FlashArgs a) {
+  using O = Ops<T, HD>;
+  constexpr int PER = 32 * kWaves;
+  __shared__ __align__(16) char tq[kRows * O::ROW], tg[kRows * O::ROW];
+  __shared__ __align__(16) float t_lse[kRows], t_delta[kRows];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5, col = lane & 31;
+  const int group = a.nq / a.nkv;
+  const int kv = blockIdx.x % a.nkv, slot = blockIdx.x / a.nkv;
+  const Span w = find_span(a.offs, a.n_seqs, a.N, slot, PER);
+  if (w.first >= w.len) return;
+  const int k0 = w.first + 32 * wave, ki = k0 + col;
+  const int64_t row = w.start + min(ki, w.len - 1);
+  typename O::Right k, v;
+  O::load_right(k, reinterpret_cast<const T*>(a.k) + row * a.ldk + kv * HD, h);
+  O::load_right(v, reinterpret_cast<const T*>(a.v) + row * a.ldv + kv * HD, h);
+  const float s2 = a.scale * kLog2e;
+  f32x16_t dk[HD / 32], dv[HD / 32];
+#pragma unroll
+  for (int d = 0; d < HD / 32; ++d) dk[d] = dv[d] = zero16();
+  for (int j = 0; j < group; ++j) {
+    const int head = kv * group + j;
+    const T* qb = reinterpret_cast<const T*>(a.q) + (int64_t)w.start * a.ldq + head * HD;
+    const T* gb = reinterpret_cast<const T*>(a.dout) + (int64_t)w.start * a.lddo + head * HD;
+    const float* lse = a.lse + (int64_t)head * a.N + w.start;
+    const float* delta = a.delta + (int64_t)head * a.N + w.start;
+    for (int m0 = w.first; m0 < w.len; m0 += kRows) {
+      __syncthreads();
+      stage<T, HD>(tq, qb + (int64_t)m0 * a.ldq, a.ldq, w.len - m0);
+      stage<T, HD>(tg, gb + (int64_t)m0 * a.lddo, a.lddo, w.len - m0);
+      for (int i = threadIdx.x; i < kRows; i += 64 * kWaves) {
+        // a row past the sequence has probability 0
+        t_lse[i] = m0 + i < w.len ? lse[m0 + i] * kLog2e : INFINITY;
+        t_delta[i] = m0 + i < w.len ? delta[m0 + i] : 0.f;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const int r0 = m0 + 32 * b;
+        if (r0 + 31 < k0) continue;
+        const f32x16_t s = O::by_rows(zero16(), tq, 32 * b, k, lane);
+        const f32x16_t dp = O::by_rows(zero16(), tg, 32 * b, v, lane);
+        const bool edge = r0 < k0 + 31;
+        float p[16], ds[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int r = result_row(i, h);
+          p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], s2, -t_lse[32 * b + r]));
+          if (edge && r0 + r < ki) p[i] = 0.f;
+          ds[i] = p[i] * (dp[i] - t_delta[32 * b + r]);
+        }
+        O::transposed(dv, tg, 32 * b, O::pack(p), lane);
+        O::transposed(dk, tq, 32 * b, O::pack(ds), lane);
+      }
+    }
+  }
+  if (ki >= w.len) return;
+  store_column<T, HD>(reinterpret_cast<T*>(a.dk) + row * a.lddk + kv * HD, dk, a.scale, h);
+  store_column<T, HD>(reinterpret_cast<T*>(a.dv) + row * a.lddv + kv * HD, dv, 1.f, h);
+}
+
+int slots_of(const FlashArgs& a, int per) { return a.N / per + a.n_seqs; }
+
+template <typename T, int HD>
+hipError_t run(const FlashArgs& a, hipStream_t st) {
+  const int group = a.nq / a.nkv, together = heads_together(group);
+  const int slots = slots_of(a, 32 * (kWaves / together));
+  flash_kernel<T, HD><<<(unsigned)(slots * (int64_t)a.nkv * (group / together)), 64 * kWaves, 0, st>>>(a, slots);
+  return hipGetLastError();
+}
+
+template <typename T, int HD>
+hipError_t run_backward(const FlashArgs& a, hipStream_t st) {
+  constexpr int ROWS = 256 / (HD / 8);
+  const int64_t items = (int64_t)a.N * a.nq;
+  flash_delta_kernel<T, HD><<<(unsigned)((items + ROWS - 1) / ROWS), 256, 0, st>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  flash_dkv_kernel<T, HD><<<(unsigned)(slots_of(a, 32 * kWaves) * (int64_t)a.nkv), 64 * kWaves, 0, st>>>(a);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int group = a.nq / a.nkv, together = heads_together(group);
+  const int slots = slots_of(a, 32 * (kWaves / together));
+  flash_dq_kernel<T, HD><<<(unsigned)(slots * (int64_t)a.nkv * (group / together)), 64 * kWaves, 0, st>>>(a, slots);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+#define TANDEM_FLASH_DISPATCH(fn)                                                            \
+  switch (hd) {                                                                              \
+    case 32: return dtype == DT_BF16 ? fn<bf16_t, 32>(a, st) : fn<float, 32>(a, st);         \
+    case 64: return dtype == DT_BF16 ? fn<bf16_t, 64>(a, st) : fn<float, 64>(a, st);         \
+    case 128: return dtype == DT_BF16 ? fn<bf16_t, 128>(a, st) : fn<float, 128>(a, st);      \
+  }                                                                                          \
+  return hipErrorInvalidValue;
+
+hipError_t launch_flash(const FlashArgs& a, int hd, int dtype, hipStream_t st) { TANDEM_FLASH_DISPATCH(run) }
+hipError_t launch_flash_backward(const FlashArgs& a, int hd, int dtype, hipStream_t st) {
+  TANDEM_FLASH_DISPATCH(run_backward)
+}
+
+}  // namespace tandem

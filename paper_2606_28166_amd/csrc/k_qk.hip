@@ -1,0 +1,254 @@
+// k_qk.hip — per-head RMSNorm of q and k with the rotary embedding in the same
+// pass, and its gradient.
+//
+// A lane holds 8 elements i .. i+7 of a head's first half and the 8 rotated with
+// them, i + h .. i + h + 7 (h = hd / 2): two 16-byte loads of bf16, no exchange for
+// the rotation, and the sums of a head run over its hd / 16 lanes.  The 8 angles of
+// a lane belong to its position, so a lane keeps them over all the heads it takes
+// of one row.  An angle is turns = position * theta^(-2i/hd) / 2 pi in 64 bits, of
+// which the fraction is left: a far position loses nothing.  Memory bound: each
+// element once in, once out (backward: two in).
+//
+// The gains' gradients are summed in a lane over its rows, then over the
+// workgroup's lanes in LDS, then over workgroups in a second launch, each in a fixed
+// order.
+#include "common.h"
+#include "update.h"
+
+namespace tandem {
+namespace {
+
+template <typename T> struct Vec8;
+template <> struct Vec8<bf16_t> {
+  u32x4_t r;
+  __device__ __forceinline__ void load(const bf16_t* p) { r = *reinterpret_cast<const u32x4_t*>(p); }
+  __device__ __forceinline__ float get(int e) const {
+    return (e & 1) ? __uint_as_float(r[e >> 1] & 0xFFFF0000u) : __uint_as_float(r[e >> 1] << 16);
+  }
+  __device__ __forceinline__ static void store(bf16_t* p, const float* v) {
+    u32x4_t r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      r[i] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * i]) |
+             ((uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * i + 1]) << 16);
+    *reinterpret_cast<u32x4_t*>(p) = r;
+  }
+};
+template <> struct Vec8<float> {
+  f32x4_t a, b;
+  __device__ __forceinline__ void load(const float* p) {
+    a = *reinterpret_cast<const f32x4_t*>(p);
+    b = *reinterpret_cast<const f32x4_t*>(p + 4);
+  }
+  __device__ __forceinline__ float get(int e) const { return e < 4 ? a[e & 3] : b[e & 3]; }
+  __device__ __forceinline__ static void store(float* p, const float* v) {
+    *reinterpret_cast<f32x4_t*>(p) = f32x4_t{v[0], v[1], v[2], v[3]};
+    *reinterpret_cast<f32x4_t*>(p + 4) = f32x4_t{v[4], v[5], v[6], v[7]};
+  }
+};
+
+// cos and sin of 2 pi turns
+__device__ __forceinline__ void turn(double turns, float* c, float* s) {
+  const float f = (float)(turns - rint(turns));      // [-1/2, 1/2]
+  sincospif(2.f * f, s, c);
+}
+
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float v) {
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
+  return v;
+}
+
+// How a workgroup's 256 threads lie on rows: LANES = hd / 16 lanes per head, `phases`
+// heads of a row side by side, the rest of the heads one after another.
+struct Place {
+  int row, head, step, lane;      // head: the first of this thread, then every step-th
+};
+template <int HD>
+__device__ __forceinline__ Place place(int phases, int block) {
+  constexpr int LANES = HD / 16;
+  const int t = threadIdx.x / LANES;
+  return Place{block * (256 / LANES / phases) + t / phases, t % phases, phases, (int)threadIdx.x % LANES};
+}
+
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void qk_kernel(QkArgs a, int phases) {
+  constexpr int H = HD / 2, LANES = HD / 16;
+  const Place w = place<HD>(phases, blockIdx.x);
+  if (w.row >= a.N) return;                  // LANES lanes of a head stay together
+  const int i0 = 8 * w.lane;
+  const double pos = (double)a.pos[w.row];
+  float c[8], s[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) turn(pos * a.turns[i0 + e], &c[e], &s[e]);
+  const T* src = reinterpret_cast<const T*>(a.qkv) + (size_t)w.row * a.ld;
+  T* q = reinterpret_cast<T*>(a.q) + (size_t)w.row * a.ldq;
+  T* k = reinterpret_cast<T*>(a.k) + (size_t)w.row * a.ldk;
+  for (int h = w.head; h < a.nq + a.nkv; h += w.step) {
+    Vec8<T> u, v;
+    u.load(src + h * HD + i0);
+    v.load(src + h * HD + H + i0);
+    float x[8], y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      x[e] = u.get(e);
+      y[e] = v.get(e);
+    }
+    if (a.gq) {
+      float q2 = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) q2 += x[e] * x[e] + y[e] * y[e];
+      const float r = 1.f / sqrtf(lanes_sum<LANES>(q2) * (1.f / HD) + a.eps);
+      const float* g = (h < a.nq ? a.gq : a.gk) + i0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        x[e] *= r * g[e];
+        y[e] *= r * g[H + e];
+      }
+    }
+    float o[8], p[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      o[e] = x[e] * c[e] - y[e] * s[e];
+      p[e] = y[e] * c[e] + x[e] * s[e];
+    }
+    T* dst = h < a.nq ? q + h * HD : k + (h - a.nq) * HD;
+    Vec8<T>::store(dst + i0, o);
+    Vec8<T>::store(dst + H + i0, p);
+  }
+}
+
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void qk_backward_kernel(QkArgs a, int phases) {
+  constexpr int H = HD / 2, LANES = HD / 16;
+  __shared__ float red[2 * HD][256 / LANES];
+  // sums of this lane's gains' gradients: [query or key][half][e]
+  float dg[2][2][8] = {};
+  const int rows = 256 / LANES / phases;     // rows of a workgroup's pass
+  for (int block = blockIdx.x; block * rows < a.N; block += gridDim.x) {
+    const Place w = place<HD>(phases, block);
+    if (w.row >= a.N) break;
+    const int i0 = 8 * w.lane;
+    const double pos = (double)a.pos[w.row];
+    float c[8], s[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) turn(pos * a.turns[i0 + e], &c[e], &s[e]);
+    const T* src = reinterpret_cast<const T*>(a.qkv) + (size_t)w.row * a.ld;
+    T* dst = reinterpret_cast<T*>(a.dqkv) + (size_t)w.row * a.ld;
+    const T* dq = reinterpret_cast<const T*>(a.dq) + (size_t)w.row * a.ldq;
+    const T* dk = reinterpret_cast<const T*>(a.dk) + (size_t)w.row * a.ldk;
+    for (int h = w.head; h < a.nq + a.nkv; h += w.step) {
+      const bool is_q = h < a.nq;
+      const T* dy = is_q ? dq + h * HD : dk + (h - a.nq) * HD;
+      Vec8<T> u, v;
+      u.load(dy + i0);
+      v.load(dy + H + i0);
+      float t[8], b[8];                      // the rotation undone: dn
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float p = u.get(e), q = v.get(e);
+        t[e] = p * c[e] + q * s[e];
+        b[e] = q * c[e] - p * s[e];
+      }
+      if (a.gq) {
+        u.load(src + h * HD + i0);
+        v.load(src + h * HD + H + i0);
+        float q2 = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) q2 += u.get(e) * u.get(e) + v.get(e) * v.get(e);
+        const float r = 1.f / sqrtf(lanes_sum<LANES>(q2) * (1.f / HD) + a.eps);
+        const float* g = (is_q ? a.gq : a.gk) + i0;
+        float tx = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float gx = t[e] * (u.get(e) * r), gy = b[e] * (v.get(e) * r);
+          dg[0][0][e] += is_q ? gx : 0.f;
+          dg[0][1][e] += is_q ? gy : 0.f;
+          dg[1][0][e] += is_q ? 0.f : gx;
+          dg[1][1][e] += is_q ? 0.f : gy;
+          t[e] *= g[e];
+          b[e] *= g[H + e];
+          tx += t[e] * u.get(e) + b[e] * v.get(e);
+        }
+        const float m = lanes_sum<LANES>(tx) * (1.f / HD) * r * r;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          t[e] = r * (t[e] - u.get(e) * m);
+          b[e] = r * (b[e] - v.get(e) * m);
+        }
+      }
+      Vec8<T>::store(dst + h * HD + i0, t);
+      Vec8<T>::store(dst + h * HD + H + i0, b);
+    }
+  }
+  if (!a.gq) return;
+  const int lane = threadIdx.x % LANES, col = threadIdx.x / LANES;
+#pragma unroll
+  for (int n = 0; n < 2; ++n)
+#pragma unroll
+    for (int f = 0; f < 2; ++f)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) red[n * HD + f * H + 8 * lane + e][col] = dg[n][f][e];
+  __syncthreads();
+  for (int i = threadIdx.x; i < 2 * HD; i += 256) {
+    float sum = 0.f;
+    for (int j = 0; j < 256 / LANES; ++j) sum += red[i][j];
+    a.part[(size_t)blockIdx.x * 2 * HD + i] = sum;
+  }
+}
+
+// The workgroups' sums, a wave per gain entry.
+__global__ __launch_bounds__(64) void qk_gain_kernel(const float* part, int blocks, int hd, float* dgq, float* dgk) {
+  const int i = blockIdx.x;
+  double sum = 0.0;
+  for (int b = threadIdx.x; b < blocks; b += kWave) sum += (double)part[(size_t)b * 2 * hd + i];
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, kWave);
+  if (threadIdx.x == 0) (i < hd ? dgq[i] : dgk[i - hd]) = (float)sum;
+}
+
+// Heads of a row side by side: a power of two that leaves each lane about four heads
+// for its angles, within one wave.
+int head_phases(int nq, int nkv, int hd) {
+  int p = 1;
+  while (2 * p * (hd / 16) <= kWave && 8 * p <= nq + nkv) p *= 2;
+  return p;
+}
+
+template <typename T, int HD>
+hipError_t run(const QkArgs& a, hipStream_t st) {
+  const int ph = head_phases(a.nq, a.nkv, HD), rows = 256 / (HD / 16) / ph;
+  qk_kernel<T, HD><<<(a.N + rows - 1) / rows, 256, 0, st>>>(a, ph);
+  return hipGetLastError();
+}
+template <typename T, int HD>
+hipError_t run_backward(const QkArgs& a, hipStream_t st) {
+  const int ph = head_phases(a.nq, a.nkv, HD), blocks = qk_backward_blocks(a.N, a.nq, a.nkv, HD);
+  qk_backward_kernel<T, HD><<<blocks, 256, 0, st>>>(a, ph);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !a.gq) return e;
+  qk_gain_kernel<<<2 * HD, 64, 0, st>>>(a.part, blocks, HD, a.dgq, a.dgk);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+int qk_backward_blocks(int N, int nq, int nkv, int hd) {
+  const int rows = 256 / (hd / 16) / head_phases(nq, nkv, hd);
+  const int most = N > 0 ? (N + rows - 1) / rows : 1;      // no rows: one workgroup writes sums of 0
+  return most < 2048 ? most : 2048;
+}
+
+#define TANDEM_QK_DISPATCH(fn)                                             \
+  switch (a.hd) {                                                          \
+    case 32: return dtype == DT_BF16 ? fn<bf16_t, 32>(a, st) : fn<float, 32>(a, st);   \
+    case 64: return dtype == DT_BF16 ? fn<bf16_t, 64>(a, st) : fn<float, 64>(a, st);   \
+    case 128: return dtype == DT_BF16 ? fn<bf16_t, 128>(a, st) : fn<float, 128>(a, st); \
+  }                                                                        \
+  return hipErrorInvalidValue;
+
+hipError_t launch_qk(const QkArgs& a, int dtype, hipStream_t st) { TANDEM_QK_DISPATCH(run) }
+hipError_t launch_qk_backward(const QkArgs& a, int dtype, hipStream_t st) { TANDEM_QK_DISPATCH(run_backward) }
+
+}  // namespace tandem

@@ -20,6 +20,7 @@
 
 #include "tandem.h"
 #include "kernels.h"
+#include "status.h"
 
 using namespace tandem;
 
@@ -904,6 +905,16 @@ tandem_status grpo_check(const tandem_grpo_cfg* c, size_t* bytes, GrpoArgs* a) {
   return TANDEM_OK;
 }
 }  // namespace
+
+namespace tandem {
+tandem_status report(tandem_status s, const char* msg) noexcept {
+  try {
+    g_err = msg;
+  } catch (...) {      // no memory for the message: the status says what it can
+  }
+  return s;
+}
+}  // namespace tandem
 
 extern "C" {
 
