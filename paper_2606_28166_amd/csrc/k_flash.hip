@@ -47,6 +47,7 @@ template <typename T, int HD> struct Ops;
 template <int HD> struct Ops<bf16_t, HD> {
   static constexpr int CPR = HD / 8;                       // chunks per row
   static constexpr int ROW = HD * 2;                       // bytes per row
+  static constexpr int WGS = 2;                            // workgroups per compute unit (registers)
   struct Right { bf16x8_t b[HD / 16]; };                   // 32 columns, summed over the head dimension
   struct Prob { bf16x8_t b[2]; };                          // 32 x 32, summed over its rows
 
@@ -99,6 +100,7 @@ template <int HD> struct Ops<bf16_t, HD> {
 template <int HD> struct Ops<float, HD> {
   static constexpr int CPR = HD / 4;
   static constexpr int ROW = HD * 4;
+  static constexpr int WGS = HD == 128 ? 1 : 2;
   struct Right { float b[HD / 2]; };
   struct Prob { float b[16]; };
 
@@ -143,17 +145,44 @@ template <int HD> struct Ops<float, HD> {
   }
 };
 
-// kRows rows from g (row stride ld elements) into a tile; rows at or past `valid` are zero.
-template <typename T, int HD>
-__device__ __forceinline__ void stage(char* tile, const T* g, int64_t ld, int valid) {
+// Where a lane's chunks of a tile lie in memory.  A load instruction of a wave fills 1 KB
+// of LDS in lane order, so the permutation of the chunks is made by the lanes' addresses;
+// the instructions of a wave are whole multiples of 8 rows apart, over which the
+// permutation repeats.
+template <typename T, int HD> struct Stager {
   using O = Ops<T, HD>;
-  constexpr int EPC = 16 / sizeof(T);
-  for (int i = threadIdx.x; i < kRows * O::CPR; i += 64 * kWaves) {
-    const int row = i / O::CPR, c = i % O::CPR;
-    u32x4_t v = {0, 0, 0, 0};
-    if (row < valid) v = *reinterpret_cast<const u32x4_t*>(g + row * ld + c * EPC);
-    *reinterpret_cast<u32x4_t*>(tile + O::at(row, c)) = v;
+  static constexpr int PER = 64 / O::CPR >= 1 ? 64 / O::CPR : 1;      // rows of one instruction
+  static constexpr int COUNT = kRows * O::CPR / (64 * kWaves);        // instructions of a wave
+  uint32_t at, step;             // bytes: this lane's chunk of the wave's first instruction, and to the next one
+  uint32_t ld;                   // bytes of a row
+  __device__ __forceinline__ Stager(int64_t stride, int lane, int wave) {
+    ld = (uint32_t)stride * sizeof(T);
+    const int chunk = 64 * wave + lane, row = chunk / O::CPR, c = chunk % O::CPR;
+    at = row * ld + ((O::at(row, c) - row * O::ROW));      // the permutation is its own inverse
+    step = kWaves * 64 / O::CPR * ld;
   }
+  // Rows 0 .. kRows-1 from g; rows at or past `valid` (>= 1) become 0.
+  __device__ __forceinline__ void load(char* tile, const T* g, int valid, int wave) const {
+    const uint32_t bytes = (uint32_t)(min(valid, kRows) - 1) * ld + HD * sizeof(T);
+    const __amdgpu_buffer_rsrc_t r = buf_rsrc(g, bytes);
+#pragma unroll
+    for (int j = 0; j < COUNT; ++j)
+      buf_load_lds16(r, tile + (wave + kWaves * j) * 1024, (int)(at + j * step), 0);
+  }
+};
+
+// kRows floats from g; entries at or past `valid` become 0.  By one wave.
+__device__ __forceinline__ void load_floats(float* dst, const float* g, int valid, int lane) {
+  const __amdgpu_buffer_rsrc_t r = buf_rsrc(g, (uint32_t)min(valid, kRows) * 4);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t*)dst, 4, lane * 4, 0, 0, 0);
+}
+
+// Everything this wave loaded has arrived, everything it read from LDS has been read; then
+// the workgroup's waves meet.
+__device__ __forceinline__ void meet() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
 }
 
 // Columns of a 32 x 32 result block row back to memory: lane (column, h) writes, per 32
@@ -191,8 +220,9 @@ __device__ __forceinline__ Span find_span(const int32_t* offs, int n_seqs, int N
   Span r = {0, 0, 0};
   if (s < 0) return r;
   s = __builtin_amdgcn_readfirstlane(s);
-  r.start = min(max(offs[s], 0), N);
-  r.len = min(max(offs[s + 1], r.start), N) - r.start;
+  // the same in every lane, and known to be: they address buffers
+  r.start = __builtin_amdgcn_readfirstlane(min(max(offs[s], 0), N));
+  r.len = __builtin_amdgcn_readfirstlane(min(max(offs[s + 1], r.start), N)) - r.start;
   r.first = (slot - (r.start / per + s)) * per;
   return r;
 }
@@ -205,36 +235,19 @@ __host__ __device__ inline int heads_together(int group) {
   return n;
 }
 
+// One tile of keys into the running softmax of a wave's 32 queries.  m2 is the maximum (in
+// powers of two) that the sums are taken against; it is raised only where a score passes
+// it by 2^8, which float32 sums and bf16's range bear, so that most tiles leave the
+// accumulator alone.
 template <typename T, int HD>
-__global__ __launch_bounds__(64 * kWaves) void flash_kernel(FlashArgs a, int slots) {
+struct Softmax {
   using O = Ops<T, HD>;
-  __shared__ __align__(16) char tk[kRows * O::ROW], tv[kRows * O::ROW];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5, col = lane & 31;
-  const int group = a.nq / a.nkv, together = heads_together(group), per = 32 * (kWaves / together);
-  const int kv = blockIdx.x % a.nkv, sub = blockIdx.x / a.nkv % (group / together);
-  // the last tiles of a sequence are its longest: they go first
-  const int slot = slots - 1 - blockIdx.x / a.nkv / (group / together);
-  const Span w = find_span(a.offs, a.n_seqs, a.N, slot, per);
-  if (w.first >= w.len) return;
-  const int head = kv * group + sub * together + wave % together;
-  const int q0 = w.first + 32 * (wave / together), qi = q0 + col;
-  const int64_t row = w.start + min(qi, w.len - 1);
-  typename O::Right q;
-  O::load_right(q, reinterpret_cast<const T*>(a.q) + row * a.ldq + head * HD, h);
-  const T* kb = reinterpret_cast<const T*>(a.k) + (int64_t)w.start * a.ldk + kv * HD;
-  const T* vb = reinterpret_cast<const T*>(a.v) + (int64_t)w.start * a.ldv + kv * HD;
-  const float s2 = a.scale * kLog2e;
-  float m = -INFINITY, l = 0.f;
+  float m2 = -INFINITY, l = 0.f;
   f32x16_t o[HD / 32];
-#pragma unroll
-  for (int d = 0; d < HD / 32; ++d) o[d] = zero16();
-  const int end = min(w.len, w.first + per);               // keys that any row of the tile sees
-  for (int n0 = 0; n0 < end; n0 += kRows) {
-    __syncthreads();
-    stage<T, HD>(tk, kb + (int64_t)n0 * a.ldk, a.ldk, w.len - n0);
-    stage<T, HD>(tv, vb + (int64_t)n0 * a.ldv, a.ldv, w.len - n0);
-    __syncthreads();
-    if (n0 > q0 + 31) continue;
+
+  __device__ __forceinline__ void tile(const char* __restrict__ tk, const char* __restrict__ tv,
+                                       const typename O::Right& q, int n0, int q0, int qi, float s2, int lane) {
+    const int h = lane >> 5;
     f32x16_t s[2];
 #pragma unroll
     for (int b = 0; b < 2; ++b) s[b] = O::by_rows(zero16(), tk, 32 * b, q, lane);
@@ -245,35 +258,75 @@ __global__ __launch_bounds__(64 * kWaves) void flash_kernel(FlashArgs a, int slo
         for (int i = 0; i < 16; ++i)
           if (n0 + 32 * b + result_row(i, h) > qi) s[b][i] = -INFINITY;
     }
-    float mx = m;
+    float mx = fmaxf(s[0][0], s[1][0]);
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, fmaxf(s[0][i], s[1][i]));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, kWave)) * s2;
+    if (__any(mx > m2 + 8.f)) {
+      const float m = fmaxf(m2, mx), f = __builtin_amdgcn_exp2f(m2 - m);
+      m2 = m;
+      l *= f;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
-    mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
-    const float f = __builtin_amdgcn_exp2f((m - mx) * s2);
-    m = mx;
-    l *= f;
-#pragma unroll
-    for (int d = 0; d < HD / 32; ++d) o[d] *= f;
+      for (int d = 0; d < HD / 32; ++d) o[d] *= f;
+    }
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       float p[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        p[i] = __builtin_amdgcn_exp2f((s[b][i] - m) * s2);
+        p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], s2, -m2));
         l += p[i];
       }
       O::transposed(o, tv, 32 * b, O::pack(p), lane);
     }
   }
-  l += __shfl_xor(l, 32, kWave);
+};
+
+template <typename T, int HD>
+__global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_kernel(FlashArgs a, int slots) {
+  using O = Ops<T, HD>;
+  constexpr int TILE = kRows * O::ROW;
+  __shared__ __align__(16) char lds[2][2][TILE];           // [turn][keys, values]
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = lane >> 5, col = lane & 31;
+  const int group = a.nq / a.nkv, together = heads_together(group), per = 32 * (kWaves / together);
+  const int kv = blockIdx.x % a.nkv, sub = blockIdx.x / a.nkv % (group / together);
+  // the last tiles of a sequence are its longest: they go first
+  const int slot = slots - 1 - blockIdx.x / a.nkv / (group / together);
+  const Span w = find_span(a.offs, a.n_seqs, a.N, slot, per);
+  if (w.first >= w.len) return;
+  const int head = kv * group + sub * together + wave % together;
+  const int q0 = w.first + 32 * (wave / together), qi = q0 + col;
+  const int64_t row = w.start + min(qi, w.len - 1);
+  const T* kb = reinterpret_cast<const T*>(a.k) + (int64_t)w.start * a.ldk + kv * HD;
+  const T* vb = reinterpret_cast<const T*>(a.v) + (int64_t)w.start * a.ldv + kv * HD;
+  const Stager<T, HD> sk(a.ldk, lane, wave), sv(a.ldv, lane, wave);
+  const int end = min(w.len, w.first + per);               // keys that any row of the tile sees
+  sk.load(lds[0][0], kb, w.len, wave);
+  sv.load(lds[0][1], vb, w.len, wave);
+  typename O::Right q;
+  O::load_right(q, reinterpret_cast<const T*>(a.q) + row * a.ldq + head * HD, h);
+  const float s2 = a.scale * kLog2e;
+  Softmax<T, HD> st;
+#pragma unroll
+  for (int d = 0; d < HD / 32; ++d) st.o[d] = zero16();
+  for (int n0 = 0, t = 0; n0 < end; n0 += kRows, t ^= 1) {
+    meet();
+    const int next = n0 + kRows;
+    if (next < end) {
+      sk.load(lds[t ^ 1][0], kb + (int64_t)next * a.ldk, w.len - next, wave);
+      sv.load(lds[t ^ 1][1], vb + (int64_t)next * a.ldv, w.len - next, wave);
+    }
+    if (n0 <= q0 + 31) st.tile(lds[t][0], lds[t][1], q, n0, q0, qi, s2, lane);
+  }
+  const float l = st.l + __shfl_xor(st.l, 32, kWave);
   if (qi >= w.len) return;
-  store_column<T, HD>(reinterpret_cast<T*>(a.out) + row * a.ldo + head * HD, o, 1.f / l, h);
-  if (h == 0) a.lse[(int64_t)head * a.N + row] = m * a.scale + logf(l);
+  store_column<T, HD>(reinterpret_cast<T*>(a.out) + row * a.ldo + head * HD, st.o, 1.f / l, h);
+  if (h == 0) a.lse[(int64_t)head * a.N + row] = (st.m2 + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-// delta[h][i] = dout_i . out_i, HD / 8 lanes per (row, head)
+// delta[h][i] = dout_i . out_i, HD / 8 lanes per (row, head), and the log-sum-exps in
+// powers of two
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void flash_delta_kernel(FlashArgs a) {
   constexpr int LANES = HD / 8;
@@ -289,14 +342,44 @@ __global__ __launch_bounds__(256) void flash_delta_kernel(FlashArgs a) {
   for (int e = 0; e < 8; ++e) s += ld(o + e) * ld(g + e);
 #pragma unroll
   for (int x = LANES / 2; x > 0; x >>= 1) s += __shfl_xor(s, x, kWave);
-  if (c == 0) a.delta[(int64_t)head * a.N + row] = s;
+  if (c == 0) {
+    const int64_t at = (int64_t)head * a.N + row;
+    a.delta[at] = s;
+    a.lse2[at] = a.lse[at] * kLog2e;
+  }
 }
 
 template <typename T, int HD>
-__global__ __launch_bounds__(64 * kWaves) void flash_dq_kernel(FlashArgs a, int slots) {
+__device__ __forceinline__ void dq_tile(f32x16_t* dq, const char* __restrict__ tk, const char* __restrict__ tv,
+                                        const typename Ops<T, HD>::Right& q, const typename Ops<T, HD>::Right& g,
+                                        int n0, int q0, int qi, float s2, float lse2, float delta, int lane) {
   using O = Ops<T, HD>;
-  __shared__ __align__(16) char tk[kRows * O::ROW], tv[kRows * O::ROW];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5, col = lane & 31;
+  const int h = lane >> 5;
+  const bool edge = n0 + kRows - 1 > q0;
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const f32x16_t s = O::by_rows(zero16(), tk, 32 * b, q, lane);
+    const f32x16_t dp = O::by_rows(zero16(), tv, 32 * b, g, lane);
+    float ds[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      ds[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], s2, -lse2)) * (dp[i] - delta);
+    if (edge) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (n0 + 32 * b + result_row(i, h) > qi) ds[i] = 0.f;
+    }
+    O::transposed(dq, tk, 32 * b, O::pack(ds), lane);
+  }
+}
+
+template <typename T, int HD>
+__global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_dq_kernel(FlashArgs a, int slots) {
+  using O = Ops<T, HD>;
+  constexpr int TILE = kRows * O::ROW;
+  __shared__ __align__(16) char lds[2][2][TILE];           // [turn][keys, values]
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = lane >> 5, col = lane & 31;
   const int group = a.nq / a.nkv, together = heads_together(group), per = 32 * (kWaves / together);
   const int kv = blockIdx.x % a.nkv, sub = blockIdx.x / a.nkv % (group / together);
   const int slot = slots - 1 - blockIdx.x / a.nkv / (group / together);
@@ -305,55 +388,88 @@ __global__ __launch_bounds__(64 * kWaves) void flash_dq_kernel(FlashArgs a, int 
   const int head = kv * group + sub * together + wave % together;
   const int q0 = w.first + 32 * (wave / together), qi = q0 + col;
   const int64_t row = w.start + min(qi, w.len - 1);
+  const T* kb = reinterpret_cast<const T*>(a.k) + (int64_t)w.start * a.ldk + kv * HD;
+  const T* vb = reinterpret_cast<const T*>(a.v) + (int64_t)w.start * a.ldv + kv * HD;
+  const Stager<T, HD> sk(a.ldk, lane, wave), sv(a.ldv, lane, wave);
+  const int end = min(w.len, w.first + per);
+  sk.load(lds[0][0], kb, w.len, wave);
+  sv.load(lds[0][1], vb, w.len, wave);
   typename O::Right q, g;
   O::load_right(q, reinterpret_cast<const T*>(a.q) + row * a.ldq + head * HD, h);
   O::load_right(g, reinterpret_cast<const T*>(a.dout) + row * a.lddo + head * HD, h);
-  const float lse = a.lse[(int64_t)head * a.N + row] * kLog2e, delta = a.delta[(int64_t)head * a.N + row];
-  const T* kb = reinterpret_cast<const T*>(a.k) + (int64_t)w.start * a.ldk + kv * HD;
-  const T* vb = reinterpret_cast<const T*>(a.v) + (int64_t)w.start * a.ldv + kv * HD;
+  const float lse2 = a.lse2[(int64_t)head * a.N + row], delta = a.delta[(int64_t)head * a.N + row];
   const float s2 = a.scale * kLog2e;
   f32x16_t dq[HD / 32];
 #pragma unroll
   for (int d = 0; d < HD / 32; ++d) dq[d] = zero16();
-  const int end = min(w.len, w.first + per);
-  for (int n0 = 0; n0 < end; n0 += kRows) {
-    __syncthreads();
-    stage<T, HD>(tk, kb + (int64_t)n0 * a.ldk, a.ldk, w.len - n0);
-    stage<T, HD>(tv, vb + (int64_t)n0 * a.ldv, a.ldv, w.len - n0);
-    __syncthreads();
-    if (n0 > q0 + 31) continue;
-    const bool edge = n0 + kRows - 1 > q0;
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const f32x16_t s = O::by_rows(zero16(), tk, 32 * b, q, lane);
-      const f32x16_t dp = O::by_rows(zero16(), tv, 32 * b, g, lane);
-      float ds[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], s2, -lse));
-        ds[i] = p * (dp[i] - delta);
-        if (edge && n0 + 32 * b + result_row(i, h) > qi) ds[i] = 0.f;
-      }
-      O::transposed(dq, tk, 32 * b, O::pack(ds), lane);
+  for (int n0 = 0, t = 0; n0 < end; n0 += kRows, t ^= 1) {
+    meet();
+    const int next = n0 + kRows;
+    if (next < end) {
+      sk.load(lds[t ^ 1][0], kb + (int64_t)next * a.ldk, w.len - next, wave);
+      sv.load(lds[t ^ 1][1], vb + (int64_t)next * a.ldv, w.len - next, wave);
     }
+    if (n0 <= q0 + 31) dq_tile<T, HD>(dq, lds[t][0], lds[t][1], q, g, n0, q0, qi, s2, lse2, delta, lane);
   }
   if (qi >= w.len) return;
   store_column<T, HD>(reinterpret_cast<T*>(a.dq) + row * a.lddq + head * HD, dq, a.scale, h);
 }
 
 template <typename T, int HD>
-__global__ __launch_bounds__(64 * kWaves) void flash_dkv_kernel(FlashArgs a) {
+__device__ __forceinline__ void dkv_tile(f32x16_t* dk, f32x16_t* dv, const char* __restrict__ tq,
+                                         const char* __restrict__ tg, const float* __restrict__ t_lse2,
+                                         const float* __restrict__ t_delta, const typename Ops<T, HD>::Right& k,
+                                         const typename Ops<T, HD>::Right& v, int m0, int k0, int ki, float s2,
+                                         int lane) {
   using O = Ops<T, HD>;
-  constexpr int PER = 32 * kWaves;
-  __shared__ __align__(16) char tq[kRows * O::ROW], tg[kRows * O::ROW];
-  __shared__ __align__(16) float t_lse[kRows], t_delta[kRows];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5, col = lane & 31;
+  const int h = lane >> 5;
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const int r0 = m0 + 32 * b;
+    if (r0 + 31 < k0) continue;
+    const f32x16_t s = O::by_rows(zero16(), tq, 32 * b, k, lane);
+    const f32x16_t dp = O::by_rows(zero16(), tg, 32 * b, v, lane);
+    float p[16], ds[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], s2, -t_lse2[32 * b + result_row(i, h)]));
+    if (r0 < k0 + 31) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (r0 + result_row(i, h) < ki) p[i] = 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) ds[i] = p[i] * (dp[i] - t_delta[32 * b + result_row(i, h)]);
+    O::transposed(dv, tg, 32 * b, O::pack(p), lane);
+    O::transposed(dk, tq, 32 * b, O::pack(ds), lane);
+  }
+}
+
+template <typename T, int HD>
+__global__ __launch_bounds__(64 * kWaves, 1) void flash_dkv_kernel(FlashArgs a) {
+  using O = Ops<T, HD>;
+  constexpr int PER = 32 * kWaves, TILE = kRows * O::ROW;
+  // a query past the sequence reads as 0, with log-sum-exp 0: probability 1 of a gradient of 0
+  __shared__ __align__(16) char lds[2][2][TILE];           // [turn][queries, output gradients]
+  __shared__ __align__(16) float stat[2][2][kRows];        // [turn][log-sum-exps, deltas]
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = lane >> 5, col = lane & 31;
   const int group = a.nq / a.nkv;
   const int kv = blockIdx.x % a.nkv, slot = blockIdx.x / a.nkv;
   const Span w = find_span(a.offs, a.n_seqs, a.N, slot, PER);
   if (w.first >= w.len) return;
   const int k0 = w.first + 32 * wave, ki = k0 + col;
   const int64_t row = w.start + min(ki, w.len - 1);
+  const Stager<T, HD> sq(a.ldq, lane, wave), sg(a.lddo, lane, wave);
+  auto load = [&](int t, int head, int m0) {
+    sq.load(lds[t][0], reinterpret_cast<const T*>(a.q) + (int64_t)(w.start + m0) * a.ldq + head * HD, w.len - m0, wave);
+    sg.load(lds[t][1], reinterpret_cast<const T*>(a.dout) + (int64_t)(w.start + m0) * a.lddo + head * HD, w.len - m0,
+            wave);
+    const int64_t at = (int64_t)head * a.N + w.start + m0;
+    if (wave == 0) load_floats(stat[t][0], a.lse2 + at, w.len - m0, lane);
+    if (wave == 1) load_floats(stat[t][1], a.delta + at, w.len - m0, lane);
+  };
+  load(0, kv * group, w.first);
   typename O::Right k, v;
   O::load_right(k, reinterpret_cast<const T*>(a.k) + row * a.ldk + kv * HD, h);
   O::load_right(v, reinterpret_cast<const T*>(a.v) + row * a.ldv + kv * HD, h);
@@ -361,41 +477,17 @@ __global__ __launch_bounds__(64 * kWaves) void flash_dkv_kernel(FlashArgs a) {
   f32x16_t dk[HD / 32], dv[HD / 32];
 #pragma unroll
   for (int d = 0; d < HD / 32; ++d) dk[d] = dv[d] = zero16();
-  for (int j = 0; j < group; ++j) {
-    const int head = kv * group + j;
-    const T* qb = reinterpret_cast<const T*>(a.q) + (int64_t)w.start * a.ldq + head * HD;
-    const T* gb = reinterpret_cast<const T*>(a.dout) + (int64_t)w.start * a.lddo + head * HD;
-    const float* lse = a.lse + (int64_t)head * a.N + w.start;
-    const float* delta = a.delta + (int64_t)head * a.N + w.start;
-    for (int m0 = w.first; m0 < w.len; m0 += kRows) {
-      __syncthreads();
-      stage<T, HD>(tq, qb + (int64_t)m0 * a.ldq, a.ldq, w.len - m0);
-      stage<T, HD>(tg, gb + (int64_t)m0 * a.lddo, a.lddo, w.len - m0);
-      for (int i = threadIdx.x; i < kRows; i += 64 * kWaves) {
-        // a row past the sequence has probability 0
-        t_lse[i] = m0 + i < w.len ? lse[m0 + i] * kLog2e : INFINITY;
-        t_delta[i] = m0 + i < w.len ? delta[m0 + i] : 0.f;
-      }
-      __syncthreads();
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const int r0 = m0 + 32 * b;
-        if (r0 + 31 < k0) continue;
-        const f32x16_t s = O::by_rows(zero16(), tq, 32 * b, k, lane);
-        const f32x16_t dp = O::by_rows(zero16(), tg, 32 * b, v, lane);
-        const bool edge = r0 < k0 + 31;
-        float p[16], ds[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int r = result_row(i, h);
-          p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], s2, -t_lse[32 * b + r]));
-          if (edge && r0 + r < ki) p[i] = 0.f;
-          ds[i] = p[i] * (dp[i] - t_delta[32 * b + r]);
-        }
-        O::transposed(dv, tg, 32 * b, O::pack(p), lane);
-        O::transposed(dk, tq, 32 * b, O::pack(ds), lane);
-      }
-    }
+  // the heads' tiles of queries, one after the other
+  const int tiles = (w.len - w.first + kRows - 1) / kRows;
+  int m0 = w.first, head = kv * group;
+  for (int i = 0, t = 0; i < group * tiles; ++i, t ^= 1) {
+    meet();
+    const bool last = m0 + kRows >= w.len;
+    const int m1 = last ? w.first : m0 + kRows, head1 = last ? head + 1 : head;
+    if (i + 1 < group * tiles) load(t ^ 1, head1, m1);
+    dkv_tile<T, HD>(dk, dv, lds[t][0], lds[t][1], stat[t][0], stat[t][1], k, v, m0, k0, ki, s2, lane);
+    m0 = m1;
+    head = head1;
   }
   if (ki >= w.len) return;
   store_column<T, HD>(reinterpret_cast<T*>(a.dk) + row * a.lddk + kv * HD, dk, a.scale, h);

@@ -114,8 +114,8 @@ tandem_status heads_check(const char* who, int32_t rows, int32_t nq, int32_t nkv
 tandem_status stride_check(const char* who, const char* what, int64_t stride, int64_t least, int32_t dtype) {
   if (stride < least) return refuse(TANDEM_E_SHAPE, "%s: %s is below a row's length", who, what);
   if (stride * elem(dtype) % 16 != 0) return refuse(TANDEM_E_ARG, "%s: %s must be a multiple of 16 bytes", who, what);
-  // a tile's rows are addressed in 31 bits from its first one
-  if (stride > (int64_t)1 << 24) return refuse(TANDEM_E_SHAPE, "%s: %s must be at most 2^24", who, what);
+  // 64 rows are addressed in 31 bits from the first
+  if (stride > (int64_t)1 << 22) return refuse(TANDEM_E_SHAPE, "%s: %s must be at most 2^22", who, what);
   return TANDEM_OK;
 }
 
@@ -321,7 +321,7 @@ tandem_status tandem_attention_workspace_size(const tandem_attention_cfg* cfg, s
   FlashArgs a;
   const tandem_status s = attention_check(who, cfg, true, &a);
   if (s != TANDEM_OK) return s;
-  *bytes = up256((size_t)a.N * a.nq * sizeof(float));
+  *bytes = 2 * up256((size_t)a.N * a.nq * sizeof(float));
   return TANDEM_OK;
 }
 
@@ -352,12 +352,13 @@ tandem_status tandem_attention_backward(const tandem_attention_cfg* cfg, const v
     return refuse(TANDEM_E_ARG, "%s: a required pointer is NULL", who);
   for (const void* p : {dout, q, k, v, out, (const void*)dq, (const void*)dk, (const void*)dv})
     if (!aligned(p, 16)) return refuse(TANDEM_E_ARG, "%s: every array must be 16-byte aligned", who);
-  const size_t need = up256((size_t)a.N * a.nq * sizeof(float));
+  const size_t need = 2 * up256((size_t)a.N * a.nq * sizeof(float));
   if ((s = check_workspace(who, workspace, workspace_bytes, need)) != TANDEM_OK) return s;
   a.q = q; a.k = k; a.v = v; a.offs = offsets;
   a.out = const_cast<void*>(out); a.lse = const_cast<float*>(lse);      // read only here
   a.dout = dout; a.dq = dq; a.dk = dk; a.dv = dv;
   a.delta = static_cast<float*>(workspace);
+  a.lse2 = reinterpret_cast<float*>(static_cast<char*>(workspace) + need / 2);
   return enqueue(who, stream, [&](hipStream_t st) { return launch_flash_backward(a, cfg->head_dim, cfg->dtype, st); });
 }
 
