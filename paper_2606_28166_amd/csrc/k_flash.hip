@@ -39,9 +39,11 @@ __device__ __forceinline__ f32x16_t zero16() {
 // row of register i in a 32 x 32 result, h = lane / 32
 __device__ __forceinline__ int result_row(int i, int h) { return 8 * (i >> 2) + 4 * h + (i & 3); }
 
-// A tile of rows of HD elements in LDS, in 16-byte chunks that are permuted by row
-// so that both readers spread over the banks: eight consecutive rows' chunks c (rows
-// as left operand) and the 32-byte pieces of four consecutive rows (transposed).
+// A tile of rows of HD elements in LDS, in 16-byte chunks whose place is permuted by row
+// (an exclusive or with `turn`) so that both readers spread over the 64 banks: 16
+// consecutive rows' chunks c (rows as left operand), and 4 rows by 64 bytes (transposed).
+// The permutation repeats after 16 rows, so a lane's places in a tile are a few offsets
+// (Lanes) plus constants.
 template <typename T, int HD> struct Ops;
 
 template <int HD> struct Ops<bf16_t, HD> {
@@ -50,10 +52,24 @@ template <int HD> struct Ops<bf16_t, HD> {
   static constexpr int WGS = 2;                            // workgroups per compute unit (registers)
   struct Right { bf16x8_t b[HD / 16]; };                   // 32 columns, summed over the head dimension
   struct Prob { bf16x8_t b[2]; };                          // 32 x 32, summed over its rows
+  struct Lanes { int rows[HD / 16], cols[2][HD / 32]; };
 
-  __device__ __forceinline__ static int at(int row, int c) {
-    const int f = CPR >= 8 ? ((row & 3) << 1) | ((row >> 2) & 1) : (((row >> 1) & 1) << 1) | ((row >> 2) & 1);
-    return row * ROW + ((c ^ f) << 4);
+  __device__ __forceinline__ static int turn(int row) {
+    return HD == 128 ? ((row & 3) << 2) | ((row >> 2) & 3)
+                     : HD == 64 ? (((row >> 1) & 1) << 2) | ((row >> 2) & 3) : (row >> 2) & 3;
+  }
+  __device__ __forceinline__ static int at(int row, int c) { return row * ROW + ((c ^ turn(row)) << 4); }
+  __device__ __forceinline__ static Lanes lanes(int lane) {
+    Lanes r;
+#pragma unroll
+    for (int k = 0; k < HD / 16; ++k) r.rows[k] = at(lane & 31, 2 * k + (lane >> 5));
+    const int g = (lane >> 4) & 1, i = lane & 15;
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+        r.cols[b][d] = at(8 * b + 4 * (lane >> 5) + (i >> 2), 4 * d + 2 * g + ((i & 3) >> 1)) + (i & 1) * 8;
+    return r;
   }
   // p: the column's row in memory
   __device__ __forceinline__ static void load_right(Right& r, const bf16_t* p, int h) {
@@ -66,34 +82,31 @@ template <int HD> struct Ops<bf16_t, HD> {
     for (int i = 0; i < 16; ++i) r.b[i >> 3][i & 7] = (__bf16)p[i];
     return r;
   }
-  // acc += tile rows r0 .. r0 + 31 by right
-  __device__ __forceinline__ static f32x16_t by_rows(f32x16_t acc, const char* tile, int r0, const Right& right,
-                                                     int lane) {
+  // tile rows r0 .. r0 + 31 by right; r0 is a multiple of 32
+  __device__ __forceinline__ static f32x16_t by_rows(const char* tile, const Lanes& at, int r0, const Right& right) {
+    f32x16_t acc = zero16();
 #pragma unroll
     for (int k = 0; k < HD / 16; ++k) {
-      const bf16x8_t a =
-          *reinterpret_cast<const bf16x8_t*>(tile + at(r0 + (lane & 31), 2 * k + (lane >> 5)));
+      const bf16x8_t a = *reinterpret_cast<const bf16x8_t*>(tile + at.rows[k] + r0 * ROW);
       acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, right.b[k], acc, 0, 0, 0);
     }
     return acc;
   }
-  // acc[d / 32] += (tile rows r0 .. r0 + 31)^T by p
-  __device__ __forceinline__ static void transposed(f32x16_t* acc, const char* tile, int r0, const Prob& p,
-                                                    int lane) {
-    const int h = lane >> 5, g = (lane >> 4) & 1, i = lane & 15;
+  // acc[d / 32] += (tile rows r0 .. r0 + 31)^T by p.  A transposing read gives a lane four
+  // positions of its dimension.
+  __device__ __forceinline__ static void transposed(f32x16_t* acc, const char* tile, const Lanes& at, int r0,
+                                                    const Prob& p) {
+    typedef short s16x8_v __attribute__((ext_vector_type(8)));
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      const int row = r0 + 16 * kb + 4 * h + (i >> 2);
+    for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
       for (int d = 0; d < HD / 32; ++d) {
-        const int c = 4 * d + 2 * g + ((i & 3) >> 1), b = (i & 1) * 8;
-        const s16x4_v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_v*)(tile + at(row, c) + b));
-        const s16x4_v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_v*)(tile + at(row + 8, c) + b));
-        typedef short s16x8_v __attribute__((ext_vector_type(8)));
+        const int to = (r0 + 16 * kb) * ROW;
+        const s16x4_v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_v*)(tile + at.cols[0][d] + to));
+        const s16x4_v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_v*)(tile + at.cols[1][d] + to));
         const s16x8_v a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), p.b[kb], acc[d], 0, 0, 0);
       }
-    }
   }
 };
 
@@ -103,8 +116,24 @@ template <int HD> struct Ops<float, HD> {
   static constexpr int WGS = HD == 128 ? 1 : 2;
   struct Right { float b[HD / 2]; };
   struct Prob { float b[16]; };
+  struct Lanes { int rows[HD / 8], cols[2][4]; };
 
-  __device__ __forceinline__ static int at(int row, int c) { return row * ROW + ((c ^ (row & 7)) << 4); }
+  __device__ __forceinline__ static int turn(int row) {
+    return HD == 32 ? (row >> 1) & 7 : (((row >> 2) & 1) << 3) | (((row >> 3) & 1) << 2) | (row & 3);
+  }
+  __device__ __forceinline__ static int at(int row, int c) { return row * ROW + ((c ^ turn(row)) << 4); }
+  __device__ __forceinline__ static Lanes lanes(int lane) {
+    Lanes r;
+    const int h = lane >> 5, c = lane & 31;
+#pragma unroll
+    for (int k = 0; k < HD / 8; ++k) r.rows[k] = at(c, h * (HD / 8) + k);
+    // row 8 b + 4 h + i, dimension c; 8 chunks on (32 dimensions) the permutation is the same
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r.cols[b][i] = at(8 * b + 4 * h + i, c >> 2) + (c & 3) * 4;
+    return r;
+  }
   __device__ __forceinline__ static void load_right(Right& r, const float* p, int h) {
 #pragma unroll
     for (int k = 0; k < HD / 8; ++k) {
@@ -119,47 +148,46 @@ template <int HD> struct Ops<float, HD> {
     for (int i = 0; i < 16; ++i) r.b[i] = p[i];
     return r;
   }
-  __device__ __forceinline__ static f32x16_t by_rows(f32x16_t acc, const char* tile, int r0, const Right& right,
-                                                     int lane) {
+  __device__ __forceinline__ static f32x16_t by_rows(const char* tile, const Lanes& at, int r0, const Right& right) {
+    f32x16_t acc = zero16();
 #pragma unroll
     for (int k = 0; k < HD / 8; ++k) {
-      const f32x4_t a =
-          *reinterpret_cast<const f32x4_t*>(tile + at(r0 + (lane & 31), (lane >> 5) * (HD / 8) + k));
+      const f32x4_t a = *reinterpret_cast<const f32x4_t*>(tile + at.rows[k] + r0 * ROW);
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], right.b[4 * k + e], acc, 0, 0, 0);
     }
     return acc;
   }
-  __device__ __forceinline__ static void transposed(f32x16_t* acc, const char* tile, int r0, const Prob& p,
-                                                    int lane) {
-    const int h = lane >> 5, c = lane & 31;
+  __device__ __forceinline__ static void transposed(f32x16_t* acc, const char* tile, const Lanes& at, int r0,
+                                                    const Prob& p) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int row = r0 + result_row(i, h);
+    for (int i = 0; i < 16; ++i)
 #pragma unroll
       for (int d = 0; d < HD / 32; ++d) {
-        const float a = *reinterpret_cast<const float*>(tile + at(row, 8 * d + (c >> 2)) + (c & 3) * 4);
+        // the chunk 8 d + c, whose exclusive or reaches its fourth bit where rows are that long
+        const int row = at.cols[(i >> 2) & 1][i & 3] + (r0 + 16 * (i >> 3)) * ROW;
+        const float a = *reinterpret_cast<const float*>(tile + (HD == 32 ? row : (row ^ ((d & 1) << 7)) + (d >> 1) * 256));
         acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p.b[i], acc[d], 0, 0, 0);
       }
-    }
   }
 };
 
 // Where a lane's chunks of a tile lie in memory.  A load instruction of a wave fills 1 KB
-// of LDS in lane order, so the permutation of the chunks is made by the lanes' addresses;
-// the instructions of a wave are whole multiples of 8 rows apart, over which the
-// permutation repeats.
+// of LDS in lane order, so the permutation of the chunks is made by the lanes' addresses,
+// one for each of a wave's instructions within 16 rows.
 template <typename T, int HD> struct Stager {
   using O = Ops<T, HD>;
-  static constexpr int PER = 64 / O::CPR >= 1 ? 64 / O::CPR : 1;      // rows of one instruction
   static constexpr int COUNT = kRows * O::CPR / (64 * kWaves);        // instructions of a wave
-  uint32_t at, step;             // bytes: this lane's chunk of the wave's first instruction, and to the next one
-  uint32_t ld;                   // bytes of a row
+  static constexpr int PASS = 64 * kWaves / O::CPR;                   // rows of one instruction of every wave
+  static constexpr int KINDS = PASS < 16 ? 16 / PASS : 1;
+  uint32_t at[KINDS], ld;        // bytes: this lane's chunks in memory; a row
   __device__ __forceinline__ Stager(int64_t stride, int lane, int wave) {
     ld = (uint32_t)stride * sizeof(T);
-    const int chunk = 64 * wave + lane, row = chunk / O::CPR, c = chunk % O::CPR;
-    at = row * ld + ((O::at(row, c) - row * O::ROW));      // the permutation is its own inverse
-    step = kWaves * 64 / O::CPR * ld;
+#pragma unroll
+    for (int j = 0; j < KINDS; ++j) {
+      const int chunk = 64 * (wave + kWaves * j) + lane, row = chunk / O::CPR, c = chunk % O::CPR;
+      at[j] = row * ld + (O::at(row, c) - row * O::ROW);   // the permutation is its own inverse
+    }
   }
   // Rows 0 .. kRows-1 from g; rows at or past `valid` (>= 1) become 0.
   __device__ __forceinline__ void load(char* tile, const T* g, int valid, int wave) const {
@@ -167,9 +195,13 @@ template <typename T, int HD> struct Stager {
     const __amdgpu_buffer_rsrc_t r = buf_rsrc(g, bytes);
 #pragma unroll
     for (int j = 0; j < COUNT; ++j)
-      buf_load_lds16(r, tile + (wave + kWaves * j) * 1024, (int)(at + j * step), 0);
+      buf_load_lds16(r, tile + (wave + kWaves * j) * 1024, (int)(at[j % KINDS] + (j / KINDS) * KINDS * PASS * ld), 0);
   }
 };
+
+// Which of the two buffers, known when the code is made: a lane's offsets then take it as a
+// constant.
+template <int N> struct Turn { static constexpr int value = N; };
 
 // kRows floats from g; entries at or past `valid` become 0.  By one wave.
 __device__ __forceinline__ void load_floats(float* dst, const float* g, int valid, int lane) {
@@ -246,11 +278,11 @@ struct Softmax {
   f32x16_t o[HD / 32];
 
   __device__ __forceinline__ void tile(const char* __restrict__ tk, const char* __restrict__ tv,
-                                       const typename O::Right& q, int n0, int q0, int qi, float s2, int lane) {
-    const int h = lane >> 5;
+                                       const typename O::Lanes& at, const typename O::Right& q, int n0, int q0,
+                                       int qi, float s2, int h) {
     f32x16_t s[2];
 #pragma unroll
-    for (int b = 0; b < 2; ++b) s[b] = O::by_rows(zero16(), tk, 32 * b, q, lane);
+    for (int b = 0; b < 2; ++b) s[b] = O::by_rows(tk, at, 32 * b, q);
     if (n0 + kRows - 1 > q0) {
 #pragma unroll
       for (int b = 0; b < 2; ++b)
@@ -277,7 +309,7 @@ struct Softmax {
         p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], s2, -m2));
         l += p[i];
       }
-      O::transposed(o, tv, 32 * b, O::pack(p), lane);
+      O::transposed(o, tv, at, 32 * b, O::pack(p));
     }
   }
 };
@@ -310,14 +342,20 @@ __global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_kernel(F
   Softmax<T, HD> st;
 #pragma unroll
   for (int d = 0; d < HD / 32; ++d) st.o[d] = zero16();
-  for (int n0 = 0, t = 0; n0 < end; n0 += kRows, t ^= 1) {
+  const typename O::Lanes at = O::lanes(lane);
+  auto step = [&](auto turn, int n0) {
+    constexpr int t = decltype(turn)::value;
     meet();
     const int next = n0 + kRows;
     if (next < end) {
       sk.load(lds[t ^ 1][0], kb + (int64_t)next * a.ldk, w.len - next, wave);
       sv.load(lds[t ^ 1][1], vb + (int64_t)next * a.ldv, w.len - next, wave);
     }
-    if (n0 <= q0 + 31) st.tile(lds[t][0], lds[t][1], q, n0, q0, qi, s2, lane);
+    if (n0 <= q0 + 31) st.tile(lds[t][0], lds[t][1], at, q, n0, q0, qi, s2, h);
+  };
+  for (int n0 = 0; n0 < end; n0 += 2 * kRows) {
+    step(Turn<0>{}, n0);
+    if (n0 + kRows < end) step(Turn<1>{}, n0 + kRows);
   }
   const float l = st.l + __shfl_xor(st.l, 32, kWave);
   if (qi >= w.len) return;
@@ -351,15 +389,15 @@ __global__ __launch_bounds__(256) void flash_delta_kernel(FlashArgs a) {
 
 template <typename T, int HD>
 __device__ __forceinline__ void dq_tile(f32x16_t* dq, const char* __restrict__ tk, const char* __restrict__ tv,
-                                        const typename Ops<T, HD>::Right& q, const typename Ops<T, HD>::Right& g,
-                                        int n0, int q0, int qi, float s2, float lse2, float delta, int lane) {
+                                        const typename Ops<T, HD>::Lanes& at, const typename Ops<T, HD>::Right& q,
+                                        const typename Ops<T, HD>::Right& g, int n0, int q0, int qi, float s2,
+                                        float lse2, float delta, int h) {
   using O = Ops<T, HD>;
-  const int h = lane >> 5;
   const bool edge = n0 + kRows - 1 > q0;
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
-    const f32x16_t s = O::by_rows(zero16(), tk, 32 * b, q, lane);
-    const f32x16_t dp = O::by_rows(zero16(), tv, 32 * b, g, lane);
+    const f32x16_t s = O::by_rows(tk, at, 32 * b, q);
+    const f32x16_t dp = O::by_rows(tv, at, 32 * b, g);
     float ds[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i)
@@ -369,7 +407,7 @@ __device__ __forceinline__ void dq_tile(f32x16_t* dq, const char* __restrict__ t
       for (int i = 0; i < 16; ++i)
         if (n0 + 32 * b + result_row(i, h) > qi) ds[i] = 0.f;
     }
-    O::transposed(dq, tk, 32 * b, O::pack(ds), lane);
+    O::transposed(dq, tk, at, 32 * b, O::pack(ds));
   }
 }
 
@@ -402,14 +440,20 @@ __global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_dq_kerne
   f32x16_t dq[HD / 32];
 #pragma unroll
   for (int d = 0; d < HD / 32; ++d) dq[d] = zero16();
-  for (int n0 = 0, t = 0; n0 < end; n0 += kRows, t ^= 1) {
+  const typename O::Lanes at = O::lanes(lane);
+  auto step = [&](auto turn, int n0) {
+    constexpr int t = decltype(turn)::value;
     meet();
     const int next = n0 + kRows;
     if (next < end) {
       sk.load(lds[t ^ 1][0], kb + (int64_t)next * a.ldk, w.len - next, wave);
       sv.load(lds[t ^ 1][1], vb + (int64_t)next * a.ldv, w.len - next, wave);
     }
-    if (n0 <= q0 + 31) dq_tile<T, HD>(dq, lds[t][0], lds[t][1], q, g, n0, q0, qi, s2, lse2, delta, lane);
+    if (n0 <= q0 + 31) dq_tile<T, HD>(dq, lds[t][0], lds[t][1], at, q, g, n0, q0, qi, s2, lse2, delta, h);
+  };
+  for (int n0 = 0; n0 < end; n0 += 2 * kRows) {
+    step(Turn<0>{}, n0);
+    if (n0 + kRows < end) step(Turn<1>{}, n0 + kRows);
   }
   if (qi >= w.len) return;
   store_column<T, HD>(reinterpret_cast<T*>(a.dq) + row * a.lddq + head * HD, dq, a.scale, h);
@@ -418,17 +462,16 @@ __global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_dq_kerne
 template <typename T, int HD>
 __device__ __forceinline__ void dkv_tile(f32x16_t* dk, f32x16_t* dv, const char* __restrict__ tq,
                                          const char* __restrict__ tg, const float* __restrict__ t_lse2,
-                                         const float* __restrict__ t_delta, const typename Ops<T, HD>::Right& k,
-                                         const typename Ops<T, HD>::Right& v, int m0, int k0, int ki, float s2,
-                                         int lane) {
+                                         const float* __restrict__ t_delta, const typename Ops<T, HD>::Lanes& at,
+                                         const typename Ops<T, HD>::Right& k, const typename Ops<T, HD>::Right& v,
+                                         int m0, int k0, int ki, float s2, int h) {
   using O = Ops<T, HD>;
-  const int h = lane >> 5;
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
     const int r0 = m0 + 32 * b;
     if (r0 + 31 < k0) continue;
-    const f32x16_t s = O::by_rows(zero16(), tq, 32 * b, k, lane);
-    const f32x16_t dp = O::by_rows(zero16(), tg, 32 * b, v, lane);
+    const f32x16_t s = O::by_rows(tq, at, 32 * b, k);
+    const f32x16_t dp = O::by_rows(tg, at, 32 * b, v);
     float p[16], ds[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i)
@@ -440,8 +483,8 @@ __device__ __forceinline__ void dkv_tile(f32x16_t* dk, f32x16_t* dv, const char*
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i) ds[i] = p[i] * (dp[i] - t_delta[32 * b + result_row(i, h)]);
-    O::transposed(dv, tg, 32 * b, O::pack(p), lane);
-    O::transposed(dk, tq, 32 * b, O::pack(ds), lane);
+    O::transposed(dv, tg, at, 32 * b, O::pack(p));
+    O::transposed(dk, tq, at, 32 * b, O::pack(ds));
   }
 }
 
@@ -480,14 +523,21 @@ __global__ __launch_bounds__(64 * kWaves, 1) void flash_dkv_kernel(FlashArgs a) 
   // the heads' tiles of queries, one after the other
   const int tiles = (w.len - w.first + kRows - 1) / kRows;
   int m0 = w.first, head = kv * group;
-  for (int i = 0, t = 0; i < group * tiles; ++i, t ^= 1) {
+  const typename O::Lanes at = O::lanes(lane);
+  auto step = [&](auto turn, bool more) {
+    constexpr int t = decltype(turn)::value;
     meet();
     const bool last = m0 + kRows >= w.len;
     const int m1 = last ? w.first : m0 + kRows, head1 = last ? head + 1 : head;
-    if (i + 1 < group * tiles) load(t ^ 1, head1, m1);
-    dkv_tile<T, HD>(dk, dv, lds[t][0], lds[t][1], stat[t][0], stat[t][1], k, v, m0, k0, ki, s2, lane);
+    if (more) load(t ^ 1, head1, m1);
+    dkv_tile<T, HD>(dk, dv, lds[t][0], lds[t][1], stat[t][0], stat[t][1], at, k, v, m0, k0, ki, s2, h);
     m0 = m1;
     head = head1;
+  };
+  const int total = group * tiles;
+  for (int i = 0; i < total; i += 2) {
+    step(Turn<0>{}, i + 1 < total);
+    if (i + 1 < total) step(Turn<1>{}, i + 2 < total);
   }
   if (ki >= w.len) return;
   store_column<T, HD>(reinterpret_cast<T*>(a.dk) + row * a.lddk + kv * HD, dk, a.scale, h);
