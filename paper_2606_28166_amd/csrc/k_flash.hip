@@ -82,9 +82,18 @@ template <int HD> struct Ops<bf16_t, HD> {
     for (int i = 0; i < 16; ++i) r.b[i >> 3][i & 7] = (__bf16)p[i];
     return r;
   }
-  // tile rows r0 .. r0 + 31 by right; r0 is a multiple of 32
-  __device__ __forceinline__ static f32x16_t by_rows(const char* tile, const Lanes& at, int r0, const Right& right) {
-    f32x16_t acc = zero16();
+  // this lane's part of the sum of a b over the head dimension
+  __device__ __forceinline__ static float dot(const Right& a, const Right& b) {
+    float s = 0.f;
+#pragma unroll
+    for (int k = 0; k < HD / 16; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s += (float)a.b[k][e] * (float)b.b[k][e];
+    return s;
+  }
+  // acc + tile rows r0 .. r0 + 31 by right; r0 is a multiple of 32
+  __device__ __forceinline__ static f32x16_t by_rows(const char* tile, const Lanes& at, int r0, const Right& right,
+                                                     f32x16_t acc = zero16()) {
 #pragma unroll
     for (int k = 0; k < HD / 16; ++k) {
       const bf16x8_t a = *reinterpret_cast<const bf16x8_t*>(tile + at.rows[k] + r0 * ROW);
@@ -148,8 +157,14 @@ template <int HD> struct Ops<float, HD> {
     for (int i = 0; i < 16; ++i) r.b[i] = p[i];
     return r;
   }
-  __device__ __forceinline__ static f32x16_t by_rows(const char* tile, const Lanes& at, int r0, const Right& right) {
-    f32x16_t acc = zero16();
+  __device__ __forceinline__ static float dot(const Right& a, const Right& b) {
+    float s = 0.f;
+#pragma unroll
+    for (int k = 0; k < HD / 2; ++k) s += a.b[k] * b.b[k];
+    return s;
+  }
+  __device__ __forceinline__ static f32x16_t by_rows(const char* tile, const Lanes& at, int r0, const Right& right,
+                                                     f32x16_t acc = zero16()) {
 #pragma unroll
     for (int k = 0; k < HD / 8; ++k) {
       const f32x4_t a = *reinterpret_cast<const f32x4_t*>(tile + at.rows[k] + r0 * ROW);
@@ -175,27 +190,27 @@ template <int HD> struct Ops<float, HD> {
 // Where a lane's chunks of a tile lie in memory.  A load instruction of a wave fills 1 KB
 // of LDS in lane order, so the permutation of the chunks is made by the lanes' addresses,
 // one for each of a wave's instructions within 16 rows.
-template <typename T, int HD> struct Stager {
+template <typename T, int HD, int ROWS = kRows, int WAVES = kWaves> struct Stager {
   using O = Ops<T, HD>;
-  static constexpr int COUNT = kRows * O::CPR / (64 * kWaves);        // instructions of a wave
-  static constexpr int PASS = 64 * kWaves / O::CPR;                   // rows of one instruction of every wave
+  static constexpr int COUNT = ROWS * O::CPR / (64 * WAVES);          // instructions of a wave
+  static constexpr int PASS = 64 * WAVES / O::CPR;                    // rows of one instruction of every wave
   static constexpr int KINDS = PASS < 16 ? 16 / PASS : 1;
   uint32_t at[KINDS], ld;        // bytes: this lane's chunks in memory; a row
   __device__ __forceinline__ Stager(int64_t stride, int lane, int wave) {
     ld = (uint32_t)stride * sizeof(T);
 #pragma unroll
     for (int j = 0; j < KINDS; ++j) {
-      const int chunk = 64 * (wave + kWaves * j) + lane, row = chunk / O::CPR, c = chunk % O::CPR;
+      const int chunk = 64 * (wave + WAVES * j) + lane, row = chunk / O::CPR, c = chunk % O::CPR;
       at[j] = row * ld + (O::at(row, c) - row * O::ROW);   // the permutation is its own inverse
     }
   }
-  // Rows 0 .. kRows-1 from g; rows at or past `valid` (>= 1) become 0.
+  // Rows 0 .. ROWS-1 from g; rows at or past `valid` (>= 1) become 0.
   __device__ __forceinline__ void load(char* tile, const T* g, int valid, int wave) const {
-    const uint32_t bytes = (uint32_t)(min(valid, kRows) - 1) * ld + HD * sizeof(T);
+    const uint32_t bytes = (uint32_t)(min(valid, ROWS) - 1) * ld + HD * sizeof(T);
     const __amdgpu_buffer_rsrc_t r = buf_rsrc(g, bytes);
 #pragma unroll
     for (int j = 0; j < COUNT; ++j)
-      buf_load_lds16(r, tile + (wave + kWaves * j) * 1024, (int)(at[j % KINDS] + (j / KINDS) * KINDS * PASS * ld), 0);
+      buf_load_lds16(r, tile + (wave + WAVES * j) * 1024, (int)(at[j % KINDS] + (j / KINDS) * KINDS * PASS * ld), 0);
   }
 };
 
@@ -203,16 +218,17 @@ template <typename T, int HD> struct Stager {
 // constant.
 template <int N> struct Turn { static constexpr int value = N; };
 
-// kRows floats from g; entries at or past `valid` become 0.  By one wave.
+// 64 floats from g; entries at or past `valid` (>= 1) become 0.  By one wave.
 __device__ __forceinline__ void load_floats(float* dst, const float* g, int valid, int lane) {
-  const __amdgpu_buffer_rsrc_t r = buf_rsrc(g, (uint32_t)min(valid, kRows) * 4);
+  const __amdgpu_buffer_rsrc_t r = buf_rsrc(g, (uint32_t)min(valid, 64) * 4);
   __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t*)dst, 4, lane * 4, 0, 0, 0);
 }
 
-// Everything this wave loaded has arrived, everything it read from LDS has been read; then
-// the workgroup's waves meet.
+// All but the LEFT newest loads of this wave have arrived, its LDS reads and writes are done;
+// then the workgroup's waves meet.
+template <int LEFT = 0>
 __device__ __forceinline__ void meet() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LEFT) : "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
@@ -363,30 +379,6 @@ __global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_kernel(F
   if (h == 0) a.lse[(int64_t)head * a.N + row] = (st.m2 + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-// delta[h][i] = dout_i . out_i, HD / 8 lanes per (row, head), and the log-sum-exps in
-// powers of two
-template <typename T, int HD>
-__global__ __launch_bounds__(256) void flash_delta_kernel(FlashArgs a) {
-  constexpr int LANES = HD / 8;
-  const int64_t item = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LANES;
-  const int c = threadIdx.x % LANES;
-  if (item >= (int64_t)a.N * a.nq) return;
-  const int64_t row = item / a.nq;
-  const int head = (int)(item % a.nq);
-  const T* o = reinterpret_cast<const T*>(a.out) + row * a.ldo + head * HD + 8 * c;
-  const T* g = reinterpret_cast<const T*>(a.dout) + row * a.lddo + head * HD + 8 * c;
-  float s = 0.f;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) s += ld(o + e) * ld(g + e);
-#pragma unroll
-  for (int x = LANES / 2; x > 0; x >>= 1) s += __shfl_xor(s, x, kWave);
-  if (c == 0) {
-    const int64_t at = (int64_t)head * a.N + row;
-    a.delta[at] = s;
-    a.lse2[at] = a.lse[at] * kLog2e;
-  }
-}
-
 template <typename T, int HD>
 __device__ __forceinline__ void dq_tile(f32x16_t* dq, const char* __restrict__ tk, const char* __restrict__ tv,
                                         const typename Ops<T, HD>::Lanes& at, const typename Ops<T, HD>::Right& q,
@@ -411,6 +403,8 @@ __device__ __forceinline__ void dq_tile(f32x16_t* dq, const char* __restrict__ t
   }
 }
 
+// dQ, and for the pass over the keys the deltas dout . out (negated) and the log-sum-exps in
+// powers of two, each (row, head) being one lane pair's.
 template <typename T, int HD>
 __global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_dq_kernel(FlashArgs a, int slots) {
   using O = Ops<T, HD>;
@@ -433,9 +427,17 @@ __global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_dq_kerne
   sk.load(lds[0][0], kb, w.len, wave);
   sv.load(lds[0][1], vb, w.len, wave);
   typename O::Right q, g;
-  O::load_right(q, reinterpret_cast<const T*>(a.q) + row * a.ldq + head * HD, h);
   O::load_right(g, reinterpret_cast<const T*>(a.dout) + row * a.lddo + head * HD, h);
-  const float lse2 = a.lse2[(int64_t)head * a.N + row], delta = a.delta[(int64_t)head * a.N + row];
+  O::load_right(q, reinterpret_cast<const T*>(a.out) + row * a.ldo + head * HD, h);
+  float delta = O::dot(g, q);
+  delta += __shfl_xor(delta, 32, kWave);
+  O::load_right(q, reinterpret_cast<const T*>(a.q) + row * a.ldq + head * HD, h);
+  const int64_t stat = (int64_t)head * a.N + row;
+  const float lse2 = a.lse[stat] * kLog2e;
+  if (h == 0 && qi < w.len) {      // for the pass over the keys
+    a.ndelta[stat] = -delta;
+    a.lse2[stat] = lse2;
+  }
   const float s2 = a.scale * kLog2e;
   f32x16_t dq[HD / 32];
 #pragma unroll
@@ -462,7 +464,7 @@ __global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_dq_kerne
 template <typename T, int HD>
 __device__ __forceinline__ void dkv_tile(f32x16_t* dk, f32x16_t* dv, const char* __restrict__ tq,
                                          const char* __restrict__ tg, const float* __restrict__ t_lse2,
-                                         const float* __restrict__ t_delta, const typename Ops<T, HD>::Lanes& at,
+                                         const float* __restrict__ t_ndelta, const typename Ops<T, HD>::Lanes& at,
                                          const typename Ops<T, HD>::Right& k, const typename Ops<T, HD>::Right& v,
                                          int m0, int k0, int ki, float s2, int h) {
   using O = Ops<T, HD>;
@@ -482,7 +484,7 @@ __device__ __forceinline__ void dkv_tile(f32x16_t* dk, f32x16_t* dv, const char*
         if (r0 + result_row(i, h) < ki) p[i] = 0.f;
     }
 #pragma unroll
-    for (int i = 0; i < 16; ++i) ds[i] = p[i] * (dp[i] - t_delta[32 * b + result_row(i, h)]);
+    for (int i = 0; i < 16; ++i) ds[i] = p[i] * (dp[i] + t_ndelta[32 * b + result_row(i, h)]);
     O::transposed(dv, tg, at, 32 * b, O::pack(p));
     O::transposed(dk, tq, at, 32 * b, O::pack(ds));
   }
@@ -494,7 +496,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void flash_dkv_kernel(FlashArgs a) 
   constexpr int PER = 32 * kWaves, TILE = kRows * O::ROW;
   // a query past the sequence reads as 0, with log-sum-exp 0: probability 1 of a gradient of 0
   __shared__ __align__(16) char lds[2][2][TILE];           // [turn][queries, output gradients]
-  __shared__ __align__(16) float stat[2][2][kRows];        // [turn][log-sum-exps, deltas]
+  __shared__ __align__(16) float stat[2][2][kRows];        // [turn][log-sum-exps, negated deltas]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = lane >> 5, col = lane & 31;
   const int group = a.nq / a.nkv;
@@ -510,7 +512,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void flash_dkv_kernel(FlashArgs a) 
             wave);
     const int64_t at = (int64_t)head * a.N + w.start + m0;
     if (wave == 0) load_floats(stat[t][0], a.lse2 + at, w.len - m0, lane);
-    if (wave == 1) load_floats(stat[t][1], a.delta + at, w.len - m0, lane);
+    if (wave == 1) load_floats(stat[t][1], a.ndelta + at, w.len - m0, lane);
   };
   load(0, kv * group, w.first);
   typename O::Right k, v;
@@ -544,6 +546,150 @@ __global__ __launch_bounds__(64 * kWaves, 1) void flash_dkv_kernel(FlashArgs a) 
   store_column<T, HD>(reinterpret_cast<T*>(a.dv) + row * a.lddv + kv * HD, dv, 1.f, h);
 }
 
+// A step of the pairs below: 32 queries by a pair's 32 keys.  The first wave's half:
+// P = e^(S - lse), dV^T += dO^T P.
+template <int HD>
+__device__ __forceinline__ void dv_step(f32x16_t* dv, const char* __restrict__ tq, const char* __restrict__ tg,
+                                        const float* __restrict__ lse2, float* __restrict__ prob,
+                                        const typename Ops<bf16_t, HD>::Lanes& at,
+                                        const typename Ops<bf16_t, HD>::Right& k, bool edge, int col, float s2, int h,
+                                        int lane) {
+  using O = Ops<bf16_t, HD>;
+  const f32x16_t s = O::by_rows(tq, at, 0, k);
+  float p[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], s2, -lse2[result_row(i, h)]));
+  if (edge) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (result_row(i, h) < col) p[i] = 0.f;
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    *reinterpret_cast<f32x4_t*>(prob + 256 * j + 4 * lane) =
+        f32x4_t{p[4 * j], p[4 * j + 1], p[4 * j + 2], p[4 * j + 3]};
+  O::transposed(dv, tg, at, 0, O::pack(p));
+}
+// The second wave's: dP - delta (the sum begins at -delta), dS = P (dP - delta), dK^T += Q^T dS.
+template <int HD>
+__device__ __forceinline__ void dk_step(f32x16_t* dk, const char* __restrict__ tq, const char* __restrict__ tg,
+                                        const float* __restrict__ ndelta, const float* __restrict__ prob,
+                                        const typename Ops<bf16_t, HD>::Lanes& at,
+                                        const typename Ops<bf16_t, HD>::Right& v, int h, int lane) {
+  using O = Ops<bf16_t, HD>;
+  f32x16_t dp;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) dp[i] = ndelta[result_row(i, h)];
+  dp = O::by_rows(tg, at, 0, v, dp);
+  float ds[16];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const f32x4_t p = *reinterpret_cast<const f32x4_t*>(prob + 256 * j + 4 * lane);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) ds[4 * j + e] = p[e] * dp[4 * j + e];
+  }
+  O::transposed(dk, tq, at, 0, O::pack(ds));
+}
+
+// dK and dV of bf16 heads of 64 and 128 by pairs of waves: of each pair's 32 keys one wave
+// forms the probabilities and dV, the other dP and dK.  Each then holds one operand and one
+// accumulator (two waves fit a SIMD, where one wave with both has it alone), and while one
+// takes exponentials the other feeds the matrix pipe.  The probabilities go through LDS in
+// float32, lane to lane, and the second wave is one step of 32 queries behind the first, so
+// that a step has one meeting.  Four tiles are in LDS: behind, current, arrived, arriving.
+template <int HD>
+__global__ __launch_bounds__(512, 2) void flash_dkv_pair_kernel(FlashArgs a) {
+  using O = Ops<bf16_t, HD>;
+  using S = Stager<bf16_t, HD, 32, 4>;
+  constexpr int TILE = 32 * O::ROW, LOADS = S::COUNT + 1;
+  __shared__ __align__(16) char lds[4][2][TILE];           // [turn][queries, output gradients]
+  __shared__ __align__(16) float prob[2][4][1024];         // [turn][pair]: probabilities in lane order
+  __shared__ __align__(16) float stat[4][8][64];           // [turn][wave]: log-sum-exps, negated deltas
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = lane >> 5, col = lane & 31, pair = wave & 3;
+  const bool second = wave >= 4;
+  const int group = a.nq / a.nkv;
+  const int kv = blockIdx.x % a.nkv, slot = blockIdx.x / a.nkv;
+  const Span w = find_span(a.offs, a.n_seqs, a.N, slot, 128);
+  if (w.first >= w.len) return;
+  const int k0 = w.first + 32 * pair, ki = k0 + col;
+  const int64_t row = w.start + min(ki, w.len - 1);
+  // the first wave holds keys, loads queries; the second holds values, loads output gradients
+  typename O::Right own;
+  O::load_right(own, second ? reinterpret_cast<const bf16_t*>(a.v) + row * a.ldv + kv * HD
+                            : reinterpret_cast<const bf16_t*>(a.k) + row * a.ldk + kv * HD, h);
+  const int64_t ld = second ? a.lddo : a.ldq;
+  const S stager(ld, lane, pair);
+  const bf16_t* src = reinterpret_cast<const bf16_t*>(second ? a.dout : a.q) + (int64_t)w.start * ld;
+  const float* src_stat = (second ? a.ndelta : a.lse2) + w.start;
+  // a step is 32 queries of one head; the heads of the group one after the other
+  const int steps = (w.len - w.first + 31) / 32, total = group * steps;
+  int lm = w.first, lhead = kv * group;                    // the next step to load
+  auto load = [&](int t) {
+    stager.load(lds[t][second ? 1 : 0], src + (int64_t)lm * ld + lhead * HD, w.len - lm, pair);
+    load_floats(stat[t][wave], src_stat + (int64_t)lhead * a.N + lm, w.len - lm, lane);
+    lm += 32;
+    if (lm >= w.len) {
+      lm = w.first;
+      ++lhead;
+    }
+  };
+  load(0);
+  if (total > 1) load(1);
+  const typename O::Lanes at = O::lanes(lane);
+  const float s2 = a.scale * kLog2e;
+  f32x16_t acc[HD / 32];
+#pragma unroll
+  for (int d = 0; d < HD / 32; ++d) acc[d] = zero16();
+  // what a step begins with: its own tile has arrived everywhere, one more may be on its way
+  auto begin = [&](int t, int i) {
+    if (i + 1 < total) meet<LOADS>();
+    else meet<0>();
+    if (i + 2 < total) load((t + 2) & 3);
+  };
+  int m0 = w.first;                                        // queries of the step at hand
+  auto next = [&]() {
+    m0 += 32;
+    if (m0 >= w.len) m0 = w.first;
+  };
+  auto first_step = [&](auto turn, int i) {
+    constexpr int t = decltype(turn)::value;
+    begin(t, i);
+    if (i >= total) return;
+    if (m0 >= k0)
+      dv_step<HD>(acc, lds[t][0], lds[t][1], stat[t][wave], prob[t & 1][pair], at, own, m0 == k0, col, s2, h, lane);
+    next();
+  };
+  auto second_step = [&](auto turn, int i) {
+    constexpr int t = decltype(turn)::value, b = (t + 3) & 3;      // the step before
+    begin(t, i);
+    if (i == 0) return;
+    if (m0 >= k0) dk_step<HD>(acc, lds[b][0], lds[b][1], stat[b][wave], prob[b & 1][pair], at, own, h, lane);
+    next();
+  };
+  // one step more than there are: the second wave's last
+  if (second) {
+    for (int i = 0; i <= total; i += 4) {
+      second_step(Turn<0>{}, i);
+      if (i + 1 <= total) second_step(Turn<1>{}, i + 1);
+      if (i + 2 <= total) second_step(Turn<2>{}, i + 2);
+      if (i + 3 <= total) second_step(Turn<3>{}, i + 3);
+    }
+  } else {
+    for (int i = 0; i <= total; i += 4) {
+      first_step(Turn<0>{}, i);
+      if (i + 1 <= total) first_step(Turn<1>{}, i + 1);
+      if (i + 2 <= total) first_step(Turn<2>{}, i + 2);
+      if (i + 3 <= total) first_step(Turn<3>{}, i + 3);
+    }
+  }
+  if (ki >= w.len) return;
+  if (second)
+    store_column<bf16_t, HD>(reinterpret_cast<bf16_t*>(a.dk) + row * a.lddk + kv * HD, acc, a.scale, h);
+  else
+    store_column<bf16_t, HD>(reinterpret_cast<bf16_t*>(a.dv) + row * a.lddv + kv * HD, acc, 1.f, h);
+}
+
 int slots_of(const FlashArgs& a, int per) { return a.N / per + a.n_seqs; }
 
 template <typename T, int HD>
@@ -556,17 +702,15 @@ hipError_t run(const FlashArgs& a, hipStream_t st) {
 
 template <typename T, int HD>
 hipError_t run_backward(const FlashArgs& a, hipStream_t st) {
-  constexpr int ROWS = 256 / (HD / 8);
-  const int64_t items = (int64_t)a.N * a.nq;
-  flash_delta_kernel<T, HD><<<(unsigned)((items + ROWS - 1) / ROWS), 256, 0, st>>>(a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  flash_dkv_kernel<T, HD><<<(unsigned)(slots_of(a, 32 * kWaves) * (int64_t)a.nkv), 64 * kWaves, 0, st>>>(a);
-  e = hipGetLastError();
-  if (e != hipSuccess) return e;
   const int group = a.nq / a.nkv, together = heads_together(group);
   const int slots = slots_of(a, 32 * (kWaves / together));
   flash_dq_kernel<T, HD><<<(unsigned)(slots * (int64_t)a.nkv * (group / together)), 64 * kWaves, 0, st>>>(a, slots);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if constexpr (sizeof(T) == 2 && HD >= 64)
+    flash_dkv_pair_kernel<HD><<<(unsigned)(slots_of(a, 128) * (int64_t)a.nkv), 512, 0, st>>>(a);
+  else
+    flash_dkv_kernel<T, HD><<<(unsigned)(slots_of(a, 32 * kWaves) * (int64_t)a.nkv), 64 * kWaves, 0, st>>>(a);
   return hipGetLastError();
 }
 

@@ -357,7 +357,7 @@ tandem_status tandem_attention_backward(const tandem_attention_cfg* cfg, const v
   a.q = q; a.k = k; a.v = v; a.offs = offsets;
   a.out = const_cast<void*>(out); a.lse = const_cast<float*>(lse);      // read only here
   a.dout = dout; a.dq = dq; a.dk = dk; a.dv = dv;
-  a.delta = static_cast<float*>(workspace);
+  a.ndelta = static_cast<float*>(workspace);
   a.lse2 = reinterpret_cast<float*>(static_cast<char*>(workspace) + need / 2);
   return enqueue(who, stream, [&](hipStream_t st) { return launch_flash_backward(a, cfg->head_dim, cfg->dtype, st); });
 }

@@ -57,7 +57,7 @@ struct FlashArgs {
   void* out; float* lse;                   // outputs of the forward pass, inputs of the backward
   const void* dout; void* dq; void* dk; void* dv;
   int64_t lddo, lddq, lddk, lddv;
-  float* delta; float* lse2;               // workspace, [nq][N] each
+  float* ndelta; float* lse2;              // workspace of the backward pass, [nq][N] each
 };
 hipError_t launch_flash(const FlashArgs& a, int hd, int dtype, hipStream_t st);
 hipError_t launch_flash_backward(const FlashArgs& a, int hd, int dtype, hipStream_t st);
