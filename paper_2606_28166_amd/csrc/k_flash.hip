@@ -82,6 +82,25 @@ template <int HD> struct Ops<bf16_t, HD> {
     for (int i = 0; i < 16; ++i) r.b[i >> 3][i & 7] = (__bf16)p[i];
     return r;
   }
+  // The order of a stretch of code with N products: a product, the reads (R) for a later one,
+  // and as much vector work (V operations, E exponentials) as its time on the matrix pipe
+  // hides.
+  template <int N, int R, int V, int E>
+  __device__ __forceinline__ static void interleave() {
+    __builtin_amdgcn_sched_group_barrier(0x100, 2 * R, 0);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, V, 0);
+      __builtin_amdgcn_sched_group_barrier(0x400, E, 0);
+    }
+  }
+  // p by a power of two: exact, but for what falls below the type's range
+  __device__ __forceinline__ static void scale(Prob& p, float by) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) p.b[i >> 3][i & 7] = (__bf16)((float)p.b[i >> 3][i & 7] * by);
+  }
   // this lane's part of the sum of a b over the head dimension
   __device__ __forceinline__ static float dot(const Right& a, const Right& b) {
     float s = 0.f;
@@ -156,6 +175,11 @@ template <int HD> struct Ops<float, HD> {
 #pragma unroll
     for (int i = 0; i < 16; ++i) r.b[i] = p[i];
     return r;
+  }
+  template <int N, int R, int V, int E> __device__ __forceinline__ static void interleave() {}
+  __device__ __forceinline__ static void scale(Prob& p, float by) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) p.b[i] *= by;
   }
   __device__ __forceinline__ static float dot(const Right& a, const Right& b) {
     float s = 0.f;
@@ -283,50 +307,71 @@ __host__ __device__ inline int heads_together(int group) {
   return n;
 }
 
-// One tile of keys into the running softmax of a wave's 32 queries.  m2 is the maximum (in
-// powers of two) that the sums are taken against; it is raised only where a score passes
-// it by 2^8, which float32 sums and bf16's range bear, so that most tiles leave the
-// accumulator alone.
+// The other half wave's value (lane l and l + 32 hold the same column).
+__device__ __forceinline__ float other_max(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// The running softmax of a wave's 32 queries over blocks of 32 keys, in three stages that
+// overlap: while the matrix pipe forms block j + 1's scores and adds block j - 1's values,
+// the vector unit takes block j's exponentials.  m2 is the maximum (in powers of two, a
+// whole number) that the sums are taken against.  It is raised only where a score passes it
+// by 2^8, which float32 sums and bf16's range bear, so that most blocks leave the
+// accumulator alone; the probabilities on their way are then scaled exactly.
 template <typename T, int HD>
 struct Softmax {
   using O = Ops<T, HD>;
-  float m2 = -INFINITY, l = 0.f;
+  float m2, l;
   f32x16_t o[HD / 32];
+  f32x16_t s;                    // block j's scores
+  typename O::Prob p;            // block j - 1's probabilities
 
-  __device__ __forceinline__ void tile(const char* __restrict__ tk, const char* __restrict__ tv,
-                                       const typename O::Lanes& at, const typename O::Right& q, int n0, int q0,
-                                       int qi, float s2, int h) {
-    f32x16_t s[2];
+  // A block's scores, its first key at n0, become block j.
+  __device__ __forceinline__ void take(const f32x16_t& next, int n0, int q0, int qi, float s2, int h) {
+    s = next;
+    if (n0 + 31 > q0) {
 #pragma unroll
-    for (int b = 0; b < 2; ++b) s[b] = O::by_rows(tk, at, 32 * b, q);
-    if (n0 + kRows - 1 > q0) {
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (n0 + 32 * b + result_row(i, h) > qi) s[b][i] = -INFINITY;
+      for (int i = 0; i < 16; ++i)
+        if (n0 + result_row(i, h) > qi) s[i] = -INFINITY;
     }
-    float mx = fmaxf(s[0][0], s[1][0]);
+    float mx = s[0];
 #pragma unroll
-    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, fmaxf(s[0][i], s[1][i]));
-    mx = fmaxf(mx, __shfl_xor(mx, 32, kWave)) * s2;
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+    mx = other_max(mx) * s2;
     if (__any(mx > m2 + 8.f)) {
-      const float m = fmaxf(m2, mx), f = __builtin_amdgcn_exp2f(m2 - m);
+      const float m = fmaxf(m2, ceilf(mx)), f = __builtin_amdgcn_exp2f(m2 - m);
       m2 = m;
       l *= f;
 #pragma unroll
       for (int d = 0; d < HD / 32; ++d) o[d] *= f;
+      O::scale(p, f);
     }
+  }
+  __device__ __forceinline__ typename O::Prob exponentials(float s2) {
+    float e[16];
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      float p[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], s2, -m2));
-        l += p[i];
-      }
-      O::transposed(o, tv, at, 32 * b, O::pack(p));
+    for (int i = 0; i < 16; ++i) {
+      e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], s2, -m2));
+      l += e[i];
     }
+    asm volatile("" : "+v"(l));    // the sum is made here, not where it is next used with 16 registers kept for it
+    return O::pack(e);
+  }
+  // Rows k0 .. of the keys' tile are block j + 1, rows v0 .. of the values' tile block j - 1.
+  __device__ __forceinline__ f32x16_t advance(const char* __restrict__ tk, int k0, const char* __restrict__ tv, int v0,
+                                              const typename O::Lanes& at, const typename O::Right& q, float s2) {
+    const f32x16_t next = O::by_rows(tk, at, k0, q);
+    O::transposed(o, tv, at, v0, p);
+    p = exponentials(s2);
+    O::template interleave<HD / 8, HD == 128 ? 2 : 2, 320 / HD + 1, 128 / HD>();
+    return next;
+  }
+  // The same at the end: no further scores.
+  __device__ __forceinline__ void drain(const char* __restrict__ tv, const typename O::Lanes& at, float s2) {
+    O::transposed(o, tv, at, 0, p);
+    p = exponentials(s2);
+    O::transposed(o, tv, at, 32, p);
   }
 };
 
@@ -350,28 +395,49 @@ __global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_kernel(F
   const T* vb = reinterpret_cast<const T*>(a.v) + (int64_t)w.start * a.ldv + kv * HD;
   const Stager<T, HD> sk(a.ldk, lane, wave), sv(a.ldv, lane, wave);
   const int end = min(w.len, w.first + per);               // keys that any row of the tile sees
-  sk.load(lds[0][0], kb, w.len, wave);
-  sv.load(lds[0][1], vb, w.len, wave);
+  const int tiles = (end + kRows - 1) / kRows;
+  const int mine = q0 < w.len ? q0 / kRows + 1 : 0;        // tiles that this wave's rows see
+  // keys run one tile ahead of values
+  auto load_k = [&](int i) { sk.load(lds[i & 1][0], kb + (int64_t)i * kRows * a.ldk, w.len - i * kRows, wave); };
+  auto load_v = [&](int i) { sv.load(lds[i & 1][1], vb + (int64_t)i * kRows * a.ldv, w.len - i * kRows, wave); };
+  load_k(0);
+  load_v(0);
+  if (tiles > 1) load_k(1);
   typename O::Right q;
   O::load_right(q, reinterpret_cast<const T*>(a.q) + row * a.ldq + head * HD, h);
   const float s2 = a.scale * kLog2e;
+  const typename O::Lanes at = O::lanes(lane);
   Softmax<T, HD> st;
+  st.m2 = -INFINITY;
+  st.l = 0.f;
 #pragma unroll
   for (int d = 0; d < HD / 32; ++d) st.o[d] = zero16();
-  const typename O::Lanes at = O::lanes(lane);
-  auto step = [&](auto turn, int n0) {
+  meet();
+  if (mine > 0) {
+    const float none[16] = {};
+    st.p = O::pack(none);
+    st.take(O::by_rows(lds[0][0], at, 0, q), 0, q0, qi, s2, h);
+    const f32x16_t second = O::by_rows(lds[0][0], at, 32, q);
+    st.p = st.exponentials(s2);
+    st.take(second, 32, q0, qi, s2, h);
+  }
+  // Step i: blocks 2 i and 2 i + 1's values (tile i), scores of tile i + 1.
+  auto step = [&](auto turn, int i) {
     constexpr int t = decltype(turn)::value;
     meet();
-    const int next = n0 + kRows;
-    if (next < end) {
-      sk.load(lds[t ^ 1][0], kb + (int64_t)next * a.ldk, w.len - next, wave);
-      sv.load(lds[t ^ 1][1], vb + (int64_t)next * a.ldv, w.len - next, wave);
+    if (i + 2 < tiles) load_k(i + 2);
+    if (i + 1 < tiles) load_v(i + 1);
+    if (i + 1 < mine) {
+      const int n0 = (i + 1) * kRows;
+      st.take(st.advance(lds[t ^ 1][0], 0, lds[t][1], 0, at, q, s2), n0, q0, qi, s2, h);
+      st.take(st.advance(lds[t ^ 1][0], 32, lds[t][1], 32, at, q, s2), n0 + 32, q0, qi, s2, h);
+    } else if (i < mine) {
+      st.drain(lds[t][1], at, s2);
     }
-    if (n0 <= q0 + 31) st.tile(lds[t][0], lds[t][1], at, q, n0, q0, qi, s2, h);
   };
-  for (int n0 = 0; n0 < end; n0 += 2 * kRows) {
-    step(Turn<0>{}, n0);
-    if (n0 + kRows < end) step(Turn<1>{}, n0 + kRows);
+  for (int i = 0; i < tiles; i += 2) {
+    step(Turn<0>{}, i);
+    if (i + 1 < tiles) step(Turn<1>{}, i + 1);
   }
   const float l = st.l + __shfl_xor(st.l, 32, kWave);
   if (qi >= w.len) return;
