@@ -228,7 +228,8 @@ template <typename T, int HD, int ROWS = kRows, int WAVES = kWaves> struct Stage
       at[j] = row * ld + (O::at(row, c) - row * O::ROW);   // the permutation is its own inverse
     }
   }
-  // Rows 0 .. ROWS-1 from g; rows at or past `valid` (>= 1) become 0.
+  // Rows 0 .. ROWS-1 from g; rows at or past `valid` (>= 1) become 0.  Callers move g along
+  // from tile to tile: a 64-bit product per tile would cost as much as a tenth of its work.
   __device__ __forceinline__ void load(char* tile, const T* g, int valid, int wave) const {
     const uint32_t bytes = (uint32_t)(min(valid, ROWS) - 1) * ld + HD * sizeof(T);
     const __amdgpu_buffer_rsrc_t r = buf_rsrc(g, bytes);
@@ -283,19 +284,20 @@ struct Span {
 };
 __device__ __forceinline__ Span find_span(const int32_t* offs, int n_seqs, int N, int slot, int per) {
   const int lane = threadIdx.x & 63;
-  int s = -1;
-  for (int b = 0; b < n_seqs; b += kWave) {
-    const int i = b + lane;
-    const int o = i < n_seqs ? min(max(offs[i], 0), N) : 0;
-    s += __popcll(__ballot(i < n_seqs && o / per + i <= slot));
-  }
   Span r = {0, 0, 0};
-  if (s < 0) return r;
-  s = __builtin_amdgcn_readfirstlane(s);
-  // the same in every lane, and known to be: they address buffers
-  r.start = __builtin_amdgcn_readfirstlane(min(max(offs[s], 0), N));
-  r.len = __builtin_amdgcn_readfirstlane(min(max(offs[s + 1], r.start), N)) - r.start;
-  r.first = (slot - (r.start / per + s)) * per;
+  // a lane per sequence, its two offsets loaded together; the last sequence that begins at
+  // or before the slot has it
+  for (int b = 0; b < n_seqs; b += kWave) {
+    const int i = min(b + lane, n_seqs - 1);
+    const int start = min(max(offs[i], 0), N), end = min(max(offs[i + 1], start), N), first = start / per + i;
+    const uint64_t at = __ballot(b + lane < n_seqs && first <= slot);
+    if (at == 0) break;
+    const int s = 63 - __builtin_clzll(at);
+    r.start = __builtin_amdgcn_readlane(start, s);
+    r.len = __builtin_amdgcn_readlane(end, s) - r.start;
+    r.first = (slot - __builtin_amdgcn_readlane(first, s)) * per;
+    if (~at != 0) break;
+  }
   return r;
 }
 
@@ -398,8 +400,15 @@ __global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_kernel(F
   const int tiles = (end + kRows - 1) / kRows;
   const int mine = q0 < w.len ? q0 / kRows + 1 : 0;        // tiles that this wave's rows see
   // keys run one tile ahead of values
-  auto load_k = [&](int i) { sk.load(lds[i & 1][0], kb + (int64_t)i * kRows * a.ldk, w.len - i * kRows, wave); };
-  auto load_v = [&](int i) { sv.load(lds[i & 1][1], vb + (int64_t)i * kRows * a.ldv, w.len - i * kRows, wave); };
+  const int64_t dk = (int64_t)kRows * a.ldk, dv = (int64_t)kRows * a.ldv;
+  auto load_k = [&](int i) {
+    sk.load(lds[i & 1][0], kb, w.len - i * kRows, wave);
+    kb += dk;
+  };
+  auto load_v = [&](int i) {
+    sv.load(lds[i & 1][1], vb, w.len - i * kRows, wave);
+    vb += dv;
+  };
   load_k(0);
   load_v(0);
   if (tiles > 1) load_k(1);
@@ -490,8 +499,14 @@ __global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_dq_kerne
   const T* vb = reinterpret_cast<const T*>(a.v) + (int64_t)w.start * a.ldv + kv * HD;
   const Stager<T, HD> sk(a.ldk, lane, wave), sv(a.ldv, lane, wave);
   const int end = min(w.len, w.first + per);
-  sk.load(lds[0][0], kb, w.len, wave);
-  sv.load(lds[0][1], vb, w.len, wave);
+  const int64_t dk = (int64_t)kRows * a.ldk, dv = (int64_t)kRows * a.ldv;
+  auto load = [&](int t, int n0) {
+    sk.load(lds[t][0], kb, w.len - n0, wave);
+    sv.load(lds[t][1], vb, w.len - n0, wave);
+    kb += dk;
+    vb += dv;
+  };
+  load(0, 0);
   typename O::Right q, g;
   O::load_right(g, reinterpret_cast<const T*>(a.dout) + row * a.lddo + head * HD, h);
   O::load_right(q, reinterpret_cast<const T*>(a.out) + row * a.ldo + head * HD, h);
@@ -512,11 +527,7 @@ __global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_dq_kerne
   auto step = [&](auto turn, int n0) {
     constexpr int t = decltype(turn)::value;
     meet();
-    const int next = n0 + kRows;
-    if (next < end) {
-      sk.load(lds[t ^ 1][0], kb + (int64_t)next * a.ldk, w.len - next, wave);
-      sv.load(lds[t ^ 1][1], vb + (int64_t)next * a.ldv, w.len - next, wave);
-    }
+    if (n0 + kRows < end) load(t ^ 1, n0 + kRows);
     if (n0 <= q0 + 31) dq_tile<T, HD>(dq, lds[t][0], lds[t][1], at, q, g, n0, q0, qi, s2, lse2, delta, h);
   };
   for (int n0 = 0; n0 < end; n0 += 2 * kRows) {
@@ -663,8 +674,11 @@ __device__ __forceinline__ void dk_step(f32x16_t* dk, const char* __restrict__ t
 // takes exponentials the other feeds the matrix pipe.  The probabilities go through LDS in
 // float32, lane to lane, and the second wave is one step of 32 queries behind the first, so
 // that a step has one meeting.  Four tiles are in LDS: behind, current, arrived, arriving.
+//
+// Where the tiles of keys are few, a workgroup takes one part of the group's heads and
+// writes float32 sums, which flash_join_kernel adds up.
 template <int HD>
-__global__ __launch_bounds__(512, 2) void flash_dkv_pair_kernel(FlashArgs a) {
+__global__ __launch_bounds__(512, 2) void flash_dkv_pair_kernel(FlashArgs a, int parts) {
   using O = Ops<bf16_t, HD>;
   using S = Stager<bf16_t, HD, 32, 4>;
   constexpr int TILE = 32 * O::ROW, LOADS = S::COUNT + 1;
@@ -674,8 +688,8 @@ __global__ __launch_bounds__(512, 2) void flash_dkv_pair_kernel(FlashArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = lane >> 5, col = lane & 31, pair = wave & 3;
   const bool second = wave >= 4;
-  const int group = a.nq / a.nkv;
-  const int kv = blockIdx.x % a.nkv, slot = blockIdx.x / a.nkv;
+  const int kv = blockIdx.x % a.nkv, part = blockIdx.x / a.nkv % parts, slot = blockIdx.x / a.nkv / parts;
+  const int group = a.nq / a.nkv / parts, head0 = kv * group * parts + part * group;
   const Span w = find_span(a.offs, a.n_seqs, a.N, slot, 128);
   if (w.first >= w.len) return;
   const int k0 = w.first + 32 * pair, ki = k0 + col;
@@ -686,18 +700,24 @@ __global__ __launch_bounds__(512, 2) void flash_dkv_pair_kernel(FlashArgs a) {
                             : reinterpret_cast<const bf16_t*>(a.k) + row * a.ldk + kv * HD, h);
   const int64_t ld = second ? a.lddo : a.ldq;
   const S stager(ld, lane, pair);
-  const bf16_t* src = reinterpret_cast<const bf16_t*>(second ? a.dout : a.q) + (int64_t)w.start * ld;
-  const float* src_stat = (second ? a.ndelta : a.lse2) + w.start;
-  // a step is 32 queries of one head; the heads of the group one after the other
+  // a step is 32 queries of one head; the heads of the part one after the other
   const int steps = (w.len - w.first + 31) / 32, total = group * steps;
-  int lm = w.first, lhead = kv * group;                    // the next step to load
+  const bf16_t* head_src = reinterpret_cast<const bf16_t*>(second ? a.dout : a.q) +
+                           (int64_t)(w.start + w.first) * ld + head0 * HD;
+  const float* head_stat = (second ? a.ndelta : a.lse2) + (int64_t)head0 * a.N + w.start + w.first;
+  const bf16_t* src = head_src;                            // of the next step to load
+  const float* src_stat = head_stat;
+  int left = w.len - w.first;                              // queries from there on
   auto load = [&](int t) {
-    stager.load(lds[t][second ? 1 : 0], src + (int64_t)lm * ld + lhead * HD, w.len - lm, pair);
-    load_floats(stat[t][wave], src_stat + (int64_t)lhead * a.N + lm, w.len - lm, lane);
-    lm += 32;
-    if (lm >= w.len) {
-      lm = w.first;
-      ++lhead;
+    stager.load(lds[t][second ? 1 : 0], src, left, pair);
+    load_floats(stat[t][wave], src_stat, left, lane);
+    src += 32 * ld;
+    src_stat += 32;
+    left -= 32;
+    if (left <= 0) {
+      left = w.len - w.first;
+      src = head_src += HD;
+      src_stat = head_stat += a.N;
     }
   };
   load(0);
@@ -750,10 +770,33 @@ __global__ __launch_bounds__(512, 2) void flash_dkv_pair_kernel(FlashArgs a) {
     }
   }
   if (ki >= w.len) return;
+  if (parts > 1) {
+    float* sums = a.sums + ((int64_t)(second ? parts : 0) + part) * a.N * a.nkv * HD;
+    store_column<float, HD>(sums + (row * a.nkv + kv) * HD, acc, second ? a.scale : 1.f, h);
+    return;
+  }
   if (second)
     store_column<bf16_t, HD>(reinterpret_cast<bf16_t*>(a.dk) + row * a.lddk + kv * HD, acc, a.scale, h);
   else
     store_column<bf16_t, HD>(reinterpret_cast<bf16_t*>(a.dv) + row * a.lddv + kv * HD, acc, 1.f, h);
+}
+
+// dV (blockIdx.y 0) and dK (1) from the parts' sums, 8 elements per thread; rows of no
+// sequence stay as they are.
+__global__ __launch_bounds__(256) void flash_join_kernel(FlashArgs a, int width, int parts) {
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8, row = i / width;
+  const int c = (int)(i % width);
+  if (row >= a.N || row < a.offs[0] || row >= a.offs[a.n_seqs]) return;
+  const int64_t plane = (int64_t)a.N * width;
+  const float* p = a.sums + (int64_t)blockIdx.y * parts * plane + i;
+  f32x4_t lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
+  for (int j = 0; j < parts; ++j, p += plane) {
+    lo += *reinterpret_cast<const f32x4_t*>(p);
+    hi += *reinterpret_cast<const f32x4_t*>(p + 4);
+  }
+  bf16_t* out = blockIdx.y ? reinterpret_cast<bf16_t*>(a.dk) + row * a.lddk : reinterpret_cast<bf16_t*>(a.dv) + row * a.lddv;
+  store4(out + c, lo[0], lo[1], lo[2], lo[3]);
+  store4(out + c + 4, hi[0], hi[1], hi[2], hi[3]);
 }
 
 int slots_of(const FlashArgs& a, int per) { return a.N / per + a.n_seqs; }
@@ -773,14 +816,30 @@ hipError_t run_backward(const FlashArgs& a, hipStream_t st) {
   flash_dq_kernel<T, HD><<<(unsigned)(slots * (int64_t)a.nkv * (group / together)), 64 * kWaves, 0, st>>>(a, slots);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if constexpr (sizeof(T) == 2 && HD >= 64)
-    flash_dkv_pair_kernel<HD><<<(unsigned)(slots_of(a, 128) * (int64_t)a.nkv), 512, 0, st>>>(a);
-  else
+  if constexpr (sizeof(T) == 2 && HD >= 64) {
+    const int parts = flash_parts(a.N, a.n_seqs, a.nq, a.nkv, HD, DT_BF16);
+    flash_dkv_pair_kernel<HD><<<(unsigned)(slots_of(a, 128) * (int64_t)a.nkv * parts), 512, 0, st>>>(a, parts);
+    if (parts > 1) {
+      const hipError_t f = hipGetLastError();
+      if (f != hipSuccess) return f;
+      const int width = a.nkv * HD;
+      flash_join_kernel<<<dim3((unsigned)(((int64_t)a.N * width / 8 + 255) / 256), 2), 256, 0, st>>>(a, width, parts);
+    }
+  } else
     flash_dkv_kernel<T, HD><<<(unsigned)(slots_of(a, 32 * kWaves) * (int64_t)a.nkv), 64 * kWaves, 0, st>>>(a);
   return hipGetLastError();
 }
 
 }  // namespace
+
+int flash_parts(int N, int n_seqs, int nq, int nkv, int hd, int dtype) {
+  // Tiles of keys differ in work by as much as a sequence is long, so it takes some three
+  // per compute unit to fill the device evenly.  With fewer, every head of the group is a
+  // part of its own: one sequence of 8703, 16 heads of 64 on 4, 769 us in 276 tiles, 362
+  // and 13 for the sums in 1104 parts.
+  const int64_t tiles = ((int64_t)N / 128 + n_seqs) * nkv;
+  return dtype == DT_BF16 && hd >= 64 && tiles < 768 ? nq / nkv : 1;
+}
 
 #define TANDEM_FLASH_DISPATCH(fn)                                                            \
   switch (hd) {                                                                              \

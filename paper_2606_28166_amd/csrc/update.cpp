@@ -168,6 +168,13 @@ tandem_status attention_check(const char* who, const tandem_attention_cfg* c, bo
   return TANDEM_OK;
 }
 
+// The backward pass's workspace: two statistics per row and head, and the sums of the parts.
+size_t attention_stat_bytes(const FlashArgs& a) { return up256((size_t)a.N * a.nq * sizeof(float)); }
+size_t attention_bytes(const FlashArgs& a, int hd, int dtype) {
+  const int parts = flash_parts(a.N, a.n_seqs, a.nq, a.nkv, hd, dtype);
+  return 2 * attention_stat_bytes(a) + (parts > 1 ? (size_t)2 * parts * a.N * a.nkv * hd * sizeof(float) : 0);
+}
+
 // ---------------------------------------------------------------- AdamW
 
 tandem_status adamw_check(const char* who, const tandem_adamw_cfg* c, const tandem_adamw_tensor* t, int32_t n,
@@ -321,7 +328,7 @@ tandem_status tandem_attention_workspace_size(const tandem_attention_cfg* cfg, s
   FlashArgs a;
   const tandem_status s = attention_check(who, cfg, true, &a);
   if (s != TANDEM_OK) return s;
-  *bytes = 2 * up256((size_t)a.N * a.nq * sizeof(float));
+  *bytes = attention_bytes(a, cfg->head_dim, cfg->dtype);
   return TANDEM_OK;
 }
 
@@ -352,13 +359,14 @@ tandem_status tandem_attention_backward(const tandem_attention_cfg* cfg, const v
     return refuse(TANDEM_E_ARG, "%s: a required pointer is NULL", who);
   for (const void* p : {dout, q, k, v, out, (const void*)dq, (const void*)dk, (const void*)dv})
     if (!aligned(p, 16)) return refuse(TANDEM_E_ARG, "%s: every array must be 16-byte aligned", who);
-  const size_t need = 2 * up256((size_t)a.N * a.nq * sizeof(float));
+  const size_t need = attention_bytes(a, cfg->head_dim, cfg->dtype);
   if ((s = check_workspace(who, workspace, workspace_bytes, need)) != TANDEM_OK) return s;
   a.q = q; a.k = k; a.v = v; a.offs = offsets;
   a.out = const_cast<void*>(out); a.lse = const_cast<float*>(lse);      // read only here
   a.dout = dout; a.dq = dq; a.dk = dk; a.dv = dv;
   a.ndelta = static_cast<float*>(workspace);
-  a.lse2 = reinterpret_cast<float*>(static_cast<char*>(workspace) + need / 2);
+  a.lse2 = reinterpret_cast<float*>(static_cast<char*>(workspace) + attention_stat_bytes(a));
+  a.sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + 2 * attention_stat_bytes(a));
   return enqueue(who, stream, [&](hipStream_t st) { return launch_flash_backward(a, cfg->head_dim, cfg->dtype, st); });
 }
 

@@ -58,7 +58,9 @@ struct FlashArgs {
   const void* dout; void* dq; void* dk; void* dv;
   int64_t lddo, lddq, lddk, lddv;
   float* ndelta; float* lse2;              // workspace of the backward pass, [nq][N] each
+  float* sums;                             // and [dV, dK][parts][N][nkv][hd], where a group's heads are cut into parts
 };
+int flash_parts(int N, int n_seqs, int nq, int nkv, int hd, int dtype);
 hipError_t launch_flash(const FlashArgs& a, int hd, int dtype, hipStream_t st);
 hipError_t launch_flash_backward(const FlashArgs& a, int hd, int dtype, hipStream_t st);
 
