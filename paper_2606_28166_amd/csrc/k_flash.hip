@@ -277,14 +277,35 @@ __device__ __forceinline__ void store_column(T* p, const f32x16_t* acc, float by
              acc[d][4 * j + 3] * by);
 }
 
-// The tile of a workgroup: sequence s owns the slots from off[s] / per + s on, one per
-// `per` positions, which are enough for it; slots past its length are empty.
+// The tile of a workgroup, `per` positions of one sequence.  Up to 64 sequences are taken by
+// length, the longest first, each one's tiles together (they read the same keys): the last
+// workgroups to start are then short ones.  With more, sequence s owns the slots from
+// off[s] / per + s on, which are enough for its tiles; the slots past its length are empty.
+// A sequence's tiles come first to last, or with `last_first` the other way round.
 struct Span {
   int start, len, first;         // first row and length of the sequence; first position of the tile (>= len: none)
 };
-__device__ __forceinline__ Span find_span(const int32_t* offs, int n_seqs, int N, int slot, int per) {
+__device__ __forceinline__ Span find_span(const int32_t* offs, int n_seqs, int N, int slot, int per, bool last_first) {
   const int lane = threadIdx.x & 63;
   Span r = {0, 0, 0};
+  if (n_seqs <= kWave) {
+    const int i = min(lane, n_seqs - 1);
+    const int start = min(max(offs[i], 0), N), end = min(max(offs[i + 1], start), N);
+    const int tiles = lane < n_seqs ? (end - start + per - 1) / per : 0;
+    int before = 0;              // tiles of the sequences ahead of this lane's
+    for (int k = 0; k < n_seqs; ++k) {
+      const int t = __builtin_amdgcn_readlane(tiles, k);
+      before += t > tiles || (t == tiles && k < lane) ? t : 0;
+    }
+    const uint64_t at = __ballot(slot >= before && slot < before + tiles);
+    if (at == 0) return r;
+    const int s = __builtin_ctzll(at), j = slot - __builtin_amdgcn_readlane(before, s);
+    r.start = __builtin_amdgcn_readlane(start, s);
+    r.len = __builtin_amdgcn_readlane(end, s) - r.start;
+    r.first = (last_first ? __builtin_amdgcn_readlane(tiles, s) - 1 - j : j) * per;
+    return r;
+  }
+  if (last_first) slot = N / per + n_seqs - 1 - slot;
   // a lane per sequence, its two offsets loaded together; the last sequence that begins at
   // or before the slot has it
   for (int b = 0; b < n_seqs; b += kWave) {
@@ -378,7 +399,7 @@ struct Softmax {
 };
 
 template <typename T, int HD>
-__global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_kernel(FlashArgs a, int slots) {
+__global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_kernel(FlashArgs a) {
   using O = Ops<T, HD>;
   constexpr int TILE = kRows * O::ROW;
   __shared__ __align__(16) char lds[2][2][TILE];           // [turn][keys, values]
@@ -387,8 +408,7 @@ __global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_kernel(F
   const int group = a.nq / a.nkv, together = heads_together(group), per = 32 * (kWaves / together);
   const int kv = blockIdx.x % a.nkv, sub = blockIdx.x / a.nkv % (group / together);
   // the last tiles of a sequence are its longest: they go first
-  const int slot = slots - 1 - blockIdx.x / a.nkv / (group / together);
-  const Span w = find_span(a.offs, a.n_seqs, a.N, slot, per);
+  const Span w = find_span(a.offs, a.n_seqs, a.N, blockIdx.x / a.nkv / (group / together), per, true);
   if (w.first >= w.len) return;
   const int head = kv * group + sub * together + wave % together;
   const int q0 = w.first + 32 * (wave / together), qi = q0 + col;
@@ -481,7 +501,7 @@ __device__ __forceinline__ void dq_tile(f32x16_t* dq, const char* __restrict__ t
 // dQ, and for the pass over the keys the deltas dout . out (negated) and the log-sum-exps in
 // powers of two, each (row, head) being one lane pair's.
 template <typename T, int HD>
-__global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_dq_kernel(FlashArgs a, int slots) {
+__global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_dq_kernel(FlashArgs a) {
   using O = Ops<T, HD>;
   constexpr int TILE = kRows * O::ROW;
   __shared__ __align__(16) char lds[2][2][TILE];           // [turn][keys, values]
@@ -489,8 +509,7 @@ __global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_dq_kerne
   const int h = lane >> 5, col = lane & 31;
   const int group = a.nq / a.nkv, together = heads_together(group), per = 32 * (kWaves / together);
   const int kv = blockIdx.x % a.nkv, sub = blockIdx.x / a.nkv % (group / together);
-  const int slot = slots - 1 - blockIdx.x / a.nkv / (group / together);
-  const Span w = find_span(a.offs, a.n_seqs, a.N, slot, per);
+  const Span w = find_span(a.offs, a.n_seqs, a.N, blockIdx.x / a.nkv / (group / together), per, true);
   if (w.first >= w.len) return;
   const int head = kv * group + sub * together + wave % together;
   const int q0 = w.first + 32 * (wave / together), qi = q0 + col;
@@ -578,7 +597,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void flash_dkv_kernel(FlashArgs a) 
   const int h = lane >> 5, col = lane & 31;
   const int group = a.nq / a.nkv;
   const int kv = blockIdx.x % a.nkv, slot = blockIdx.x / a.nkv;
-  const Span w = find_span(a.offs, a.n_seqs, a.N, slot, PER);
+  const Span w = find_span(a.offs, a.n_seqs, a.N, slot, PER, false);
   if (w.first >= w.len) return;
   const int k0 = w.first + 32 * wave, ki = k0 + col;
   const int64_t row = w.start + min(ki, w.len - 1);
@@ -690,7 +709,7 @@ __global__ __launch_bounds__(512, 2) void flash_dkv_pair_kernel(FlashArgs a, int
   const bool second = wave >= 4;
   const int kv = blockIdx.x % a.nkv, part = blockIdx.x / a.nkv % parts, slot = blockIdx.x / a.nkv / parts;
   const int group = a.nq / a.nkv / parts, head0 = kv * group * parts + part * group;
-  const Span w = find_span(a.offs, a.n_seqs, a.N, slot, 128);
+  const Span w = find_span(a.offs, a.n_seqs, a.N, slot, 128, false);
   if (w.first >= w.len) return;
   const int k0 = w.first + 32 * pair, ki = k0 + col;
   const int64_t row = w.start + min(ki, w.len - 1);
@@ -805,7 +824,7 @@ template <typename T, int HD>
 hipError_t run(const FlashArgs& a, hipStream_t st) {
   const int group = a.nq / a.nkv, together = heads_together(group);
   const int slots = slots_of(a, 32 * (kWaves / together));
-  flash_kernel<T, HD><<<(unsigned)(slots * (int64_t)a.nkv * (group / together)), 64 * kWaves, 0, st>>>(a, slots);
+  flash_kernel<T, HD><<<(unsigned)(slots * (int64_t)a.nkv * (group / together)), 64 * kWaves, 0, st>>>(a);
   return hipGetLastError();
 }
 
@@ -813,7 +832,7 @@ template <typename T, int HD>
 hipError_t run_backward(const FlashArgs& a, hipStream_t st) {
   const int group = a.nq / a.nkv, together = heads_together(group);
   const int slots = slots_of(a, 32 * (kWaves / together));
-  flash_dq_kernel<T, HD><<<(unsigned)(slots * (int64_t)a.nkv * (group / together)), 64 * kWaves, 0, st>>>(a, slots);
+  flash_dq_kernel<T, HD><<<(unsigned)(slots * (int64_t)a.nkv * (group / together)), 64 * kWaves, 0, st>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if constexpr (sizeof(T) == 2 && HD >= 64) {
