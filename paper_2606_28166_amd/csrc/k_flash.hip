@@ -258,8 +258,6 @@ __device__ __forceinline__ void meet() {
   asm volatile("" ::: "memory");
 }
 
-// Columns of a 32 x 32 result block row back to memory: lane (column, h) writes, per 32
-// dimensions, four runs of four.
 __device__ __forceinline__ void store4(bf16_t* p, float a, float b, float c, float d) {
   typedef __bf16 bf16x4_v __attribute__((ext_vector_type(4)));
   *reinterpret_cast<bf16x4_v*>(p) = bf16x4_v{(__bf16)a, (__bf16)b, (__bf16)c, (__bf16)d};
@@ -267,14 +265,29 @@ __device__ __forceinline__ void store4(bf16_t* p, float a, float b, float c, flo
 __device__ __forceinline__ void store4(float* p, float a, float b, float c, float d) {
   *reinterpret_cast<f32x4_t*>(p) = f32x4_t{a, b, c, d};
 }
+// The 32 columns of a wave's result, times `by`, as rows of memory: `valid` rows from g.  A lane
+// holds parts of one row; through LDS (32 rows of this wave's own, laid out as a tile) they
+// go out in whole rows.
 template <typename T, int HD>
-__device__ __forceinline__ void store_column(T* p, const f32x16_t* acc, float by, int h) {
+__device__ __forceinline__ void store_rows(char* own, T* g, int64_t ld, int valid, const f32x16_t* acc, float by,
+                                           int lane) {
+  using O = Ops<T, HD>;
+  constexpr int EPC = 16 / sizeof(T);
+  const int h = lane >> 5, col = lane & 31;
 #pragma unroll
   for (int d = 0; d < HD / 32; ++d)
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      store4(p + 32 * d + 8 * j + 4 * h, acc[d][4 * j] * by, acc[d][4 * j + 1] * by, acc[d][4 * j + 2] * by,
-             acc[d][4 * j + 3] * by);
+    for (int j = 0; j < 4; ++j) {
+      const int e = 32 * d + 8 * j + 4 * h;
+      store4(reinterpret_cast<T*>(own + O::at(col, e / EPC)) + e % EPC, acc[d][4 * j] * by, acc[d][4 * j + 1] * by,
+             acc[d][4 * j + 2] * by, acc[d][4 * j + 3] * by);
+    }
+#pragma unroll
+  for (int n = 0; n < 32 * O::CPR / 64; ++n) {
+    const int p = 64 * n + lane, row = p / O::CPR, c = p % O::CPR;
+    const u32x4_t v = *reinterpret_cast<const u32x4_t*>(own + O::at(row, c));
+    if (row < valid) *reinterpret_cast<u32x4_t*>(g + row * ld + c * EPC) = v;
+  }
 }
 
 // The tile of a workgroup, `per` positions of one sequence.  Up to 64 sequences are taken by
@@ -469,9 +482,11 @@ __global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_kernel(F
     if (i + 1 < tiles) step(Turn<1>{}, i + 1);
   }
   const float l = st.l + __shfl_xor(st.l, 32, kWave);
-  if (qi >= w.len) return;
-  store_column<T, HD>(reinterpret_cast<T*>(a.out) + row * a.ldo + head * HD, st.o, 1.f / l, h);
-  if (h == 0) a.lse[(int64_t)head * a.N + row] = (st.m2 + __builtin_amdgcn_logf(l)) * kLn2;
+  meet();                                                  // the tiles' room takes the results
+  if (mine == 0) return;
+  store_rows<T, HD>(lds[0][0] + wave * 32 * O::ROW, reinterpret_cast<T*>(a.out) + (int64_t)(w.start + q0) * a.ldo + head * HD,
+                    a.ldo, w.len - q0, st.o, 1.f / l, lane);
+  if (h == 0 && qi < w.len) a.lse[(int64_t)head * a.N + row] = (st.m2 + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 template <typename T, int HD>
@@ -553,8 +568,10 @@ __global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_dq_kerne
     step(Turn<0>{}, n0);
     if (n0 + kRows < end) step(Turn<1>{}, n0 + kRows);
   }
-  if (qi >= w.len) return;
-  store_column<T, HD>(reinterpret_cast<T*>(a.dq) + row * a.lddq + head * HD, dq, a.scale, h);
+  meet();                                                  // the tiles' room takes the results
+  if (q0 >= w.len) return;
+  store_rows<T, HD>(lds[0][0] + wave * 32 * O::ROW, reinterpret_cast<T*>(a.dq) + (int64_t)(w.start + q0) * a.lddq + head * HD,
+                    a.lddq, w.len - q0, dq, a.scale, lane);
 }
 
 template <typename T, int HD>
@@ -637,9 +654,12 @@ __global__ __launch_bounds__(64 * kWaves, 1) void flash_dkv_kernel(FlashArgs a) 
     step(Turn<0>{}, i + 1 < total);
     if (i + 1 < total) step(Turn<1>{}, i + 2 < total);
   }
-  if (ki >= w.len) return;
-  store_column<T, HD>(reinterpret_cast<T*>(a.dk) + row * a.lddk + kv * HD, dk, a.scale, h);
-  store_column<T, HD>(reinterpret_cast<T*>(a.dv) + row * a.lddv + kv * HD, dv, 1.f, h);
+  meet();                                                  // the tiles' room takes the results
+  if (k0 >= w.len) return;
+  char* room = lds[0][0] + wave * 32 * O::ROW;
+  const int64_t row0 = w.start + k0;
+  store_rows<T, HD>(room, reinterpret_cast<T*>(a.dk) + row0 * a.lddk + kv * HD, a.lddk, w.len - k0, dk, a.scale, lane);
+  store_rows<T, HD>(room, reinterpret_cast<T*>(a.dv) + row0 * a.lddv + kv * HD, a.lddv, w.len - k0, dv, 1.f, lane);
 }
 
 // A step of the pairs below: 32 queries by a pair's 32 keys.  The first wave's half:
@@ -687,9 +707,20 @@ __device__ __forceinline__ void dk_step(f32x16_t* dk, const char* __restrict__ t
   O::transposed(dk, tq, at, 0, O::pack(ds));
 }
 
+// A lane's column of a result, float32, 16 bytes at a time.
+template <int HD>
+__device__ __forceinline__ void store_column(float* p, const f32x16_t* acc, float by, int h) {
+#pragma unroll
+  for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      store4(p + 32 * d + 8 * j + 4 * h, acc[d][4 * j] * by, acc[d][4 * j + 1] * by, acc[d][4 * j + 2] * by,
+             acc[d][4 * j + 3] * by);
+}
+
 // dK and dV of bf16 heads of 64 and 128 by pairs of waves: of each pair's 32 keys one wave
 // forms the probabilities and dV, the other dP and dK.  Each then holds one operand and one
-// accumulator (two waves fit a SIMD, where one wave with both has it alone), and while one
+// accumulator (of heads of 128 two waves fit a SIMD, where one wave with both has it alone; of 64 four), and while one
 // takes exponentials the other feeds the matrix pipe.  The probabilities go through LDS in
 // float32, lane to lane, and the second wave is one step of 32 queries behind the first, so
 // that a step has one meeting.  Four tiles are in LDS: behind, current, arrived, arriving.
@@ -697,7 +728,7 @@ __device__ __forceinline__ void dk_step(f32x16_t* dk, const char* __restrict__ t
 // Where the tiles of keys are few, a workgroup takes one part of the group's heads and
 // writes float32 sums, which flash_join_kernel adds up.
 template <int HD>
-__global__ __launch_bounds__(512, 2) void flash_dkv_pair_kernel(FlashArgs a, int parts) {
+__global__ __launch_bounds__(512, (HD == 64 ? 4 : 2)) void flash_dkv_pair_kernel(FlashArgs a, int parts) {
   using O = Ops<bf16_t, HD>;
   using S = Stager<bf16_t, HD, 32, 4>;
   constexpr int TILE = 32 * O::ROW, LOADS = S::COUNT + 1;
@@ -788,16 +819,20 @@ __global__ __launch_bounds__(512, 2) void flash_dkv_pair_kernel(FlashArgs a, int
       if (i + 3 <= total) first_step(Turn<3>{}, i + 3);
     }
   }
-  if (ki >= w.len) return;
+  meet();                                                  // the tiles' room takes the results
+  if (k0 >= w.len) return;
+  const int64_t row0 = w.start + k0;
+  const float by = second ? a.scale : 1.f;
   if (parts > 1) {
-    float* sums = a.sums + ((int64_t)(second ? parts : 0) + part) * a.N * a.nkv * HD;
-    store_column<float, HD>(sums + (row * a.nkv + kv) * HD, acc, second ? a.scale : 1.f, h);
+    float* sums = a.sums + (((int64_t)(second ? parts : 0) + part) * a.N + row0) * a.nkv * HD + kv * HD;
+    if (ki < w.len) store_column<HD>(sums + (int64_t)(lane & 31) * a.nkv * HD, acc, by, h);
     return;
   }
+  char* room = lds[0][0] + wave * 32 * O::ROW;
   if (second)
-    store_column<bf16_t, HD>(reinterpret_cast<bf16_t*>(a.dk) + row * a.lddk + kv * HD, acc, a.scale, h);
+    store_rows<bf16_t, HD>(room, reinterpret_cast<bf16_t*>(a.dk) + row0 * a.lddk + kv * HD, a.lddk, w.len - k0, acc, by, lane);
   else
-    store_column<bf16_t, HD>(reinterpret_cast<bf16_t*>(a.dv) + row * a.lddv + kv * HD, acc, 1.f, h);
+    store_rows<bf16_t, HD>(room, reinterpret_cast<bf16_t*>(a.dv) + row0 * a.lddv + kv * HD, a.lddv, w.len - k0, acc, by, lane);
 }
 
 // dV (blockIdx.y 0) and dK (1) from the parts' sums, 8 elements per thread; rows of no
