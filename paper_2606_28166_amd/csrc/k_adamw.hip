@@ -95,6 +95,11 @@ __global__ __launch_bounds__(NT) void adamw_norm_kernel(AdamwArgs a) {
   if (threadIdx.x == 0) a.part[blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
 }
 
+__device__ __forceinline__ float clip_factor(double norm, double max_norm) {
+  const double c = max_norm / (norm + 1e-6);
+  return c >= 1.0 ? 1.f : (float)c;          // a NaN stays
+}
+
 // One workgroup: the norm and the clipping factor.
 __global__ __launch_bounds__(1024) void adamw_clip_kernel(const double* part, int chunks, double max_norm,
                                                           float* norm, float* clip) {
@@ -110,8 +115,7 @@ __global__ __launch_bounds__(1024) void adamw_clip_kernel(const double* part, in
     for (int w = 0; w < 1024 / kWave; ++w) sum += red[w];
     const double n = sqrt(sum);
     norm[0] = (float)n;
-    const double c = max_norm / (n + 1e-6);
-    clip[0] = c < 1.0 ? (float)c : (c >= 1.0 ? 1.f : (float)c);      // a NaN stays
+    clip[0] = clip_factor(n, max_norm);
   }
 }
 
@@ -121,7 +125,20 @@ __global__ __launch_bounds__(NT) void adamw_kernel(AdamwArgs a) {
   const bool p16 = (a.p16[ti >> 6] >> (ti & 63)) & 1, g16 = (a.g16[ti >> 6] >> (ti & 63)) & 1;
   const int64_t i0 = (int64_t)(blockIdx.x - t.first) * kAdamwChunk;
   const int64_t i1 = i0 + kAdamwChunk < t.n ? i0 + kAdamwChunk : t.n;
-  const float clip = a.clip ? *a.clip : 1.f;
+  float clip = a.clip ? *a.clip : 1.f;
+  if (a.few > 0) {
+    // A small model: a launch less.  The same sum in the same order in every workgroup.
+    __shared__ double red[NT / kWave];
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < a.few; i += NT) sum += a.part[i];
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, kWave);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x / kWave] = sum;
+    __syncthreads();
+    const double n = sqrt((red[0] + red[1]) + (red[2] + red[3]));
+    clip = clip_factor(n, a.max_norm);
+    if (a.norm && blockIdx.x == 0 && threadIdx.x == 0) a.norm[0] = (float)n;
+  }
   float* m = a.m + t.off;
   float* v = a.v + t.off;
   // the weights are read from their master copies where there are any

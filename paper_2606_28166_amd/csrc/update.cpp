@@ -405,7 +405,9 @@ tandem_status tandem_adamw(const tandem_adamw_cfg* cfg, const tandem_adamw_tenso
     a.lr = (float)cfg->lr; a.eps = (float)cfg->eps;
     a.inv_bc1 = (float)(1.0 / (1.0 - std::pow(cfg->beta1, cfg->step)));
     a.inv_bc2 = (float)(1.0 / (1.0 - std::pow(cfg->beta2, cfg->step)));
-    a.clip = clipped ? clip : nullptr;
+    a.few = clipped && chunks <= kAdamwFew ? (int)chunks : 0;
+    a.clip = clipped && !a.few ? clip : nullptr;
+    a.max_norm = cfg->max_norm;
     // pass 0 (with clipping): the sums of squares; pass 1: the update
     for (int pass = clipped ? 0 : 1; pass < 2; ++pass) {
       int64_t before = 0;                     // chunks of earlier launches
@@ -426,12 +428,14 @@ tandem_status tandem_adamw(const tandem_adamw_cfg* cfg, const tandem_adamw_tenso
           ++a.n;
         }
         if (grid == 0) continue;
-        a.part = part + before;
+        // the update's launches all read the sums from the first on, and one of them reports the norm
+        a.part = pass == 0 ? part + before : part;
+        a.norm = a.few && before == 0 ? norm : nullptr;
         before += grid;
         const hipError_t e = pass == 0 ? launch_adamw_norm(a, (int)grid, st) : launch_adamw(a, (int)grid, st);
         if (e != hipSuccess) return e;
       }
-      if (pass == 0) {
+      if (pass == 0 && (!a.few || before == 0)) {
         const hipError_t e = launch_adamw_clip(part, (int)before, cfg->max_norm, norm, clip, st);
         if (e != hipSuccess) return e;
       }

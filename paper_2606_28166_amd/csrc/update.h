@@ -75,12 +75,15 @@ struct AdamwTensor {
 // most 4 KB, and nothing has to be uploaded.
 constexpr int kAdamwTensors = 96;
 constexpr int kAdamwChunk = 8192;          // elements per workgroup
+constexpr int kAdamwFew = 512;             // chunks whose sums every workgroup of the update can add up
 struct AdamwArgs {
   float* m; float* v; float* master;
   float b1, c1, b2, c2;                    // betas and 1 - beta
   float lr, inv_bc1, inv_bc2, eps;         // 1 / (1 - beta^t)
-  const float* clip;                       // device scalar c, or NULL (c = 1)
+  const float* clip;                       // device scalar c, or NULL (c = 1, or from few chunks' sums)
   double* part;                            // sums of squares by chunk
+  int few;                                 // > 0: the update adds up that many chunks' sums itself
+  float* norm; double max_norm;            // of the update then: norm NULL in all launches but the first
   int n;                                   // tensors of this launch
   uint64_t p16[2], g16[2];                 // bit i: tensor i's weights / gradient are bf16
   AdamwTensor t[kAdamwTensors];

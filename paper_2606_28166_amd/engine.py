@@ -212,35 +212,59 @@ def grpo_loss(rewards: torch.Tensor, owner: torch.Tensor, length: torch.Tensor, 
 # Each function below runs on the current torch stream of its tensors' device and
 # returns device tensors; a forward function's dict is what its backward function
 # takes.  Gradients are computed by explicit backward functions, there is no autograd
-# graph.
+# graph.  A small call is bound by the host, so the checks are few comparisons per tensor
+# and outputs of one kind share an allocation.
 
 _DT = {torch.bfloat16: L.BF16, torch.float32: L.F32}
+_lib = L.lib
 
 
 def _same(who: str, name: str, t: torch.Tensor, dtype, shape, dev) -> None:
     """A contiguous tensor of this dtype, shape and device."""
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != dev or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or t.device != dev or not t.is_contiguous():
         raise ValueError(f"{who}: {name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {dev}")
 
 
 def _rows(who: str, name: str, t: torch.Tensor, dtype, shape, dev) -> int:
     """The row stride of a tensor whose rows are contiguous ([rows, ...])."""
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != dev:
+    if t.dtype is not dtype or t.shape != shape or t.device != dev:
         raise ValueError(f"{who}: {name} must be a {dtype} tensor of shape {tuple(shape)} on {dev}")
+    stride = t.stride()
     width = 1
-    for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
-        if size != 1 and stride != width:
+    for i in range(len(stride) - 1, 0, -1):
+        size = shape[i]
+        if stride[i] != width and size != 1:
             raise ValueError(f"{who}: the rows of {name} must be contiguous")
         width *= size
     # one row: any stride does
-    return t.stride(0) if t.shape[0] > 1 else width
+    return stride[0] if shape[0] > 1 else width
 
 
-def _on(dev):
-    """The current stream of dev; a CPU device is refused here, before its memory reaches a kernel."""
+def _gpu(dev) -> None:
+    """Refuses a CPU device before its memory reaches a kernel."""
     if dev.type != "cuda":
         raise ValueError(f"tensors must be on a GPU, got {dev}")
-    return torch.cuda.current_stream(dev).cuda_stream
+
+
+def _run(dev, fn, *args) -> None:
+    """fn(*args, the current stream of dev), with dev current."""
+    index = dev.index
+    if torch._C._cuda_getDevice() != index:
+        with torch.cuda.device(dev):
+            L.check(fn(*args, torch._C._cuda_getCurrentRawStream(index)))
+        return
+    status = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+    if status != L.OK:
+        L.check(status)
+
+
+def _need(fn, *args) -> int:
+    """The workspace that a *_workspace_size call asks for."""
+    n = C.c_size_t()
+    status = fn(*args, n)
+    if status != L.OK:
+        L.check(status)
+    return n.value
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -257,15 +281,16 @@ def _workspace(t: Optional[torch.Tensor], need: int, dev) -> Optional[torch.Tens
 
 
 def _logprob_cfg(who, logits, tokens, ref, temperature, eos_id, eos_bias, eos_bias_ref):
-    if logits.dim() != 2 or logits.dtype not in _DT:
+    dt = logits.dtype
+    if logits.dim() != 2 or dt not in _DT:
         raise ValueError(f"{who}: logits must be a bfloat16 or float32 tensor [rows][vocab]")
-    R, V = logits.shape
-    _on(logits.device)
-    ld = _rows(who, "logits", logits, logits.dtype, (R, V), logits.device)
-    ldr = _rows(who, "ref", ref, logits.dtype, (R, V), logits.device) if ref is not None else V
-    _same(who, "tokens", tokens, torch.int32, (R,), logits.device)
-    return L.LogprobCfg(R, V, _DT[logits.dtype], int(eos_id), ld, ldr, V, float(temperature), float(eos_bias),
-                        float(eos_bias_ref))
+    shape, dev = logits.shape, logits.device
+    R, V = shape
+    _gpu(dev)
+    ld = _rows(who, "logits", logits, dt, shape, dev)
+    ldr = _rows(who, "ref", ref, dt, shape, dev) if ref is not None else V
+    _same(who, "tokens", tokens, torch.int32, (R,), dev)
+    return L.LogprobCfg(R, V, _DT[dt], eos_id, ld, ldr, V, temperature, eos_bias, eos_bias_ref), dev
 
 
 def token_logprob(logits: torch.Tensor, tokens: torch.Tensor, ref: Optional[torch.Tensor] = None,
@@ -277,16 +302,21 @@ def token_logprob(logits: torch.Tensor, tokens: torch.Tensor, ref: Optional[torc
     from, (z + eos_bias e_eos) / temperature.  Tokens outside the vocabulary
     (-1: padding) leave their row out.  Returns logp, lse, kl, lse_diff, each
     float32 [R] (the last two None without ref)."""
-    cfg = _logprob_cfg("token_logprob", logits, tokens, ref, temperature, eos_id, eos_bias, eos_bias_ref)
-    dev, R = logits.device, logits.shape[0]
-    need = L.tandem_logprob_workspace_size(cfg)
+    cfg, dev = _logprob_cfg("token_logprob", logits, tokens, ref, temperature, eos_id, eos_bias, eos_bias_ref)
+    R = cfg.rows
+    need = _need(_lib.tandem_logprob_workspace_size, cfg)
     workspace = _workspace(workspace, need, dev)
     out = torch.empty((4 if ref is not None else 2, R), dtype=torch.float32, device=dev)
-    kl, diff = (out[2], out[3]) if ref is not None else (None, None)
-    with torch.cuda.device(dev):
-        L.tandem_token_logprob(cfg, logits.data_ptr(), _ptr(ref), tokens.data_ptr(), out[0].data_ptr(),
-                               out[1].data_ptr(), _ptr(kl), _ptr(diff), _ptr(workspace), need, _on(dev))
-    return dict(logp=out[0], lse=out[1], kl=kl, lse_diff=diff)
+    p = out.data_ptr()
+    if ref is not None:
+        _run(dev, _lib.tandem_token_logprob, cfg, logits.data_ptr(), ref.data_ptr(), tokens.data_ptr(), p, p + 4 * R,
+             p + 8 * R, p + 12 * R, _ptr(workspace), need)
+        logp, lse, kl, diff = out.unbind(0)
+        return dict(logp=logp, lse=lse, kl=kl, lse_diff=diff)
+    _run(dev, _lib.tandem_token_logprob, cfg, logits.data_ptr(), None, tokens.data_ptr(), p, p + 4 * R, None, None,
+         _ptr(workspace), need)
+    logp, lse = out.unbind(0)
+    return dict(logp=logp, lse=lse, kl=None, lse_diff=None)
 
 
 def token_logprob_backward(logits: torch.Tensor, tokens: torch.Tensor, fwd, g_logp: torch.Tensor,
@@ -297,37 +327,44 @@ def token_logprob_backward(logits: torch.Tensor, tokens: torch.Tensor, fwd, g_lo
     logits' dtype; fwd is what token_logprob returned for the same arguments.
     out may be logits itself: the gradient then takes its place."""
     who = "token_logprob_backward"
-    cfg = _logprob_cfg(who, logits, tokens, ref, temperature, eos_id, eos_bias, eos_bias_ref)
-    dev, (R, V) = logits.device, logits.shape
-    if g_kl is not None and (ref is None or fwd["kl"] is None):
-        raise ValueError(f"{who}: g_kl needs ref, in the forward pass too")
-    for name, t in (("g_logp", g_logp), ("g_kl", g_kl), ("fwd['lse']", fwd["lse"]),
-                    ("fwd['kl']", fwd["kl"] if g_kl is not None else None),
-                    ("fwd['lse_diff']", fwd["lse_diff"] if g_kl is not None else None)):
-        if t is not None:
-            _same(who, name, t, torch.float32, (R,), dev)
+    cfg, dev = _logprob_cfg(who, logits, tokens, ref, temperature, eos_id, eos_bias, eos_bias_ref)
+    row = (cfg.rows,)
+    lse, kl, diff = fwd["lse"], None, None
+    _same(who, "g_logp", g_logp, torch.float32, row, dev)
+    _same(who, "fwd['lse']", lse, torch.float32, row, dev)
+    if g_kl is not None:
+        kl, diff = fwd["kl"], fwd["lse_diff"]
+        if ref is None or kl is None:
+            raise ValueError(f"{who}: g_kl needs ref, in the forward pass too")
+        _same(who, "g_kl", g_kl, torch.float32, row, dev)
+        _same(who, "fwd['kl']", kl, torch.float32, row, dev)
+        _same(who, "fwd['lse_diff']", diff, torch.float32, row, dev)
+    else:
+        ref = None
     if out is None:
-        out = torch.empty((R, V), dtype=logits.dtype, device=dev)
-    cfg.grad_stride = _rows(who, "out", out, logits.dtype, (R, V), dev)
-    kl, diff = (fwd["kl"], fwd["lse_diff"]) if g_kl is not None else (None, None)
-    with torch.cuda.device(dev):
-        L.tandem_token_logprob_backward(cfg, logits.data_ptr(), _ptr(ref if g_kl is not None else None),
-                                        tokens.data_ptr(), fwd["lse"].data_ptr(), _ptr(kl), _ptr(diff),
-                                        g_logp.data_ptr(), _ptr(g_kl), out.data_ptr(), _on(dev))
+        out = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+    else:
+        cfg.grad_stride = _rows(who, "out", out, logits.dtype, logits.shape, dev)
+    _run(dev, _lib.tandem_token_logprob_backward, cfg, logits.data_ptr(), _ptr(ref), tokens.data_ptr(),
+         lse.data_ptr(), _ptr(kl), _ptr(diff), g_logp.data_ptr(), _ptr(g_kl), out.data_ptr())
     return out
 
 
 def _qk_cfg(who, qkv, positions, n_q, n_kv, theta, eps, q_gain, k_gain):
-    if qkv.dim() != 2 or qkv.dtype not in _DT or qkv.shape[1] % (n_q + 2 * n_kv) != 0:
+    dt, dev = qkv.dtype, qkv.device
+    if qkv.dim() != 2 or dt not in _DT or n_q < 1 or n_kv < 1 or qkv.shape[1] % (n_q + 2 * n_kv) != 0:
         raise ValueError(f"{who}: qkv must be a bfloat16 or float32 tensor [rows][(n_q + 2 n_kv) * head_dim]")
-    N, hd = qkv.shape[0], qkv.shape[1] // (n_q + 2 * n_kv)
-    _on(qkv.device)
-    ld = _rows(who, "qkv", qkv, qkv.dtype, qkv.shape, qkv.device)
-    _same(who, "positions", positions, torch.int32, (N,), qkv.device)
-    for name, t in (("q_gain", q_gain), ("k_gain", k_gain)):
-        if t is not None:
-            _same(who, name, t, torch.float32, (hd,), qkv.device)
-    return L.QkCfg(N, n_q, n_kv, hd, _DT[qkv.dtype], float(theta), float(eps), ld, n_q * hd, n_kv * hd)
+    N, cols = qkv.shape
+    hd = cols // (n_q + 2 * n_kv)
+    _gpu(dev)
+    ld = _rows(who, "qkv", qkv, dt, qkv.shape, dev)
+    _same(who, "positions", positions, torch.int32, (N,), dev)
+    if (q_gain is None) != (k_gain is None):
+        raise ValueError(f"{who}: q_gain and k_gain go together")
+    if q_gain is not None:
+        _same(who, "q_gain", q_gain, torch.float32, (hd,), dev)
+        _same(who, "k_gain", k_gain, torch.float32, (hd,), dev)
+    return L.QkCfg(N, n_q, n_kv, hd, _DT[dt], theta, eps, ld, n_q * hd, n_kv * hd), dev
 
 
 def qk_norm_rope(qkv: torch.Tensor, positions: torch.Tensor, n_q: int, n_kv: int, theta: float, eps: float,
@@ -336,15 +373,14 @@ def qk_norm_rope(qkv: torch.Tensor, positions: torch.Tensor, n_q: int, n_kv: int
     heads of a packed QKV projection [N][(n_q + 2 n_kv) * head_dim] at
     positions int32 [N] (tandem_qk_norm_rope).  Returns q [N][n_q][head_dim],
     k [N][n_kv][head_dim] and v, a view of the value columns."""
-    who = "qk_norm_rope"
-    cfg = _qk_cfg(who, qkv, positions, n_q, n_kv, theta, eps, q_gain, k_gain)
-    N, hd, dev = cfg.rows, cfg.head_dim, qkv.device
+    cfg, dev = _qk_cfg("qk_norm_rope", qkv, positions, n_q, n_kv, theta, eps, q_gain, k_gain)
+    N, hd = cfg.rows, cfg.head_dim
     q = torch.empty((N, n_q, hd), dtype=qkv.dtype, device=dev)
     k = torch.empty((N, n_kv, hd), dtype=qkv.dtype, device=dev)
-    with torch.cuda.device(dev):
-        L.tandem_qk_norm_rope(cfg, qkv.data_ptr(), _ptr(q_gain), _ptr(k_gain), positions.data_ptr(), q.data_ptr(),
-                              k.data_ptr(), _on(dev))
-    return dict(q=q, k=k, v=qkv[:, (n_q + n_kv) * hd:].unflatten(1, (n_kv, hd)))
+    _run(dev, _lib.tandem_qk_norm_rope, cfg, qkv.data_ptr(), _ptr(q_gain), _ptr(k_gain), positions.data_ptr(),
+         q.data_ptr(), k.data_ptr())
+    v = qkv.as_strided((N, n_kv, hd), (qkv.stride(0), hd, 1), qkv.storage_offset() + (n_q + n_kv) * hd)
+    return dict(q=q, k=k, v=v)
 
 
 def qk_norm_rope_backward(qkv: torch.Tensor, positions: torch.Tensor, dq: torch.Tensor, dk: torch.Tensor,
@@ -360,41 +396,45 @@ def qk_norm_rope_backward(qkv: torch.Tensor, positions: torch.Tensor, dq: torch.
     if dq.dim() != 3 or dk.dim() != 3:
         raise ValueError(f"{who}: dq and dk must be [rows][heads][head_dim]")
     n_q, n_kv = dq.shape[1], dk.shape[1]
-    cfg = _qk_cfg(who, qkv, positions, n_q, n_kv, theta, eps, q_gain, k_gain)
-    N, hd, dev = cfg.rows, cfg.head_dim, qkv.device
-    cfg.q_stride = _rows(who, "dq", dq, qkv.dtype, (N, n_q, hd), dev)
-    cfg.k_stride = _rows(who, "dk", dk, qkv.dtype, (N, n_kv, hd), dev)
+    cfg, dev = _qk_cfg(who, qkv, positions, n_q, n_kv, theta, eps, q_gain, k_gain)
+    N, hd, dt = cfg.rows, cfg.head_dim, qkv.dtype
+    cfg.q_stride = _rows(who, "dq", dq, dt, (N, n_q, hd), dev)
+    cfg.k_stride = _rows(who, "dk", dk, dt, (N, n_kv, hd), dev)
     if dqkv is None:
-        dqkv = torch.empty_strided(qkv.shape, (cfg.qkv_stride, 1), dtype=qkv.dtype, device=dev)
+        dqkv = torch.empty_strided(qkv.shape, (cfg.qkv_stride, 1), dtype=dt, device=dev)
         dqkv[:, (n_q + n_kv) * hd:].zero_()
-    elif _rows(who, "dqkv", dqkv, qkv.dtype, qkv.shape, dev) != cfg.qkv_stride:
+    elif _rows(who, "dqkv", dqkv, dt, qkv.shape, dev) != cfg.qkv_stride:
         raise ValueError(f"{who}: dqkv must have the strides of qkv")
-    if (q_gain is None) != (k_gain is None):
-        raise ValueError(f"{who}: q_gain and k_gain go together")
-    gain = torch.empty((2, hd), dtype=torch.float32, device=dev) if q_gain is not None else None
-    need = L.tandem_qk_workspace_size(cfg) if q_gain is not None else 0
+    if q_gain is None:
+        _run(dev, _lib.tandem_qk_norm_rope_backward, cfg, qkv.data_ptr(), None, None, positions.data_ptr(),
+             dq.data_ptr(), dk.data_ptr(), dqkv.data_ptr(), None, None, None, 0)
+        return dict(dqkv=dqkv, dq_gain=None, dk_gain=None)
+    gain = torch.empty((2, hd), dtype=torch.float32, device=dev)
+    p = gain.data_ptr()
+    need = _need(_lib.tandem_qk_workspace_size, cfg)
     workspace = _workspace(workspace, need, dev)
-    dgq, dgk = (gain[0], gain[1]) if gain is not None else (None, None)
-    with torch.cuda.device(dev):
-        L.tandem_qk_norm_rope_backward(cfg, qkv.data_ptr(), _ptr(q_gain), _ptr(k_gain), positions.data_ptr(),
-                                       dq.data_ptr(), dk.data_ptr(), dqkv.data_ptr(), _ptr(dgq), _ptr(dgk),
-                                       _ptr(workspace), need, _on(dev))
+    _run(dev, _lib.tandem_qk_norm_rope_backward, cfg, qkv.data_ptr(), q_gain.data_ptr(), k_gain.data_ptr(),
+         positions.data_ptr(), dq.data_ptr(), dk.data_ptr(), dqkv.data_ptr(), p, p + 4 * hd, workspace.data_ptr(), need)
+    dgq, dgk = gain.unbind(0)
     return dict(dqkv=dqkv, dq_gain=dgq, dk_gain=dgk)
 
 
 def _attention_cfg(who, q, k, v, offsets, scale):
-    if q.dim() != 3 or k.dim() != 3 or q.dtype not in _DT:
+    dt, dev = q.dtype, q.device
+    if q.dim() != 3 or k.dim() != 3 or dt not in _DT:
         raise ValueError(f"{who}: q and k must be bfloat16 or float32 tensors [rows][heads][head_dim]")
-    (N, nq, hd), nkv, dev = q.shape, k.shape[1], q.device
-    _on(dev)
+    _gpu(dev)
+    N, nq, hd = q.shape
+    nkv = k.shape[1]
+    heads = (N, nkv, hd)
     if offsets.dim() != 1 or offsets.numel() < 1:
         raise ValueError(f"{who}: offsets must hold at least one entry")
     _same(who, "offsets", offsets, torch.int32, offsets.shape, dev)
-    return L.AttentionCfg(N, offsets.numel() - 1, nq, nkv, hd, _DT[q.dtype],
-                          float(scale) if scale is not None else hd ** -0.5,
-                          _rows(who, "q", q, q.dtype, q.shape, dev), _rows(who, "k", k, q.dtype, (N, nkv, hd), dev),
-                          _rows(who, "v", v, q.dtype, (N, nkv, hd), dev), nq * hd, nq * hd, nq * hd, nkv * hd,
-                          nkv * hd)
+    qs, ks = nq * hd, nkv * hd
+    return L.AttentionCfg(N, offsets.numel() - 1, nq, nkv, hd, _DT[dt],
+                          scale if scale is not None else hd ** -0.5 if hd > 0 else 0.0,
+                          _rows(who, "q", q, dt, q.shape, dev), _rows(who, "k", k, dt, heads, dev),
+                          _rows(who, "v", v, dt, heads, dev), qs, qs, qs, ks, ks), dt, dev
 
 
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets: torch.Tensor,
@@ -404,15 +444,14 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets: torch.
     [N][n_q][head_dim], k and v [N][n_kv][head_dim] are sequence s.  scale:
     1 / sqrt(head_dim) by default.  Returns out [N][n_q][head_dim] and lse
     float32 [n_q][N]; rows that belong to no sequence are not written."""
-    who = "attention"
-    cfg = _attention_cfg(who, q, k, v, offsets, scale)
+    cfg, dt, dev = _attention_cfg("attention", q, k, v, offsets, scale)
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    cfg.out_stride = _rows(who, "out", out, q.dtype, q.shape, q.device)
-    lse = torch.empty((cfg.n_q_heads, cfg.rows), dtype=torch.float32, device=q.device)
-    with torch.cuda.device(q.device):
-        L.tandem_attention(cfg, q.data_ptr(), k.data_ptr(), v.data_ptr(), offsets.data_ptr(), out.data_ptr(),
-                           lse.data_ptr(), _on(q.device))
+        out = torch.empty(q.shape, dtype=dt, device=dev)
+    else:
+        cfg.out_stride = _rows("attention", "out", out, dt, q.shape, dev)
+    lse = torch.empty((cfg.n_q_heads, cfg.rows), dtype=torch.float32, device=dev)
+    _run(dev, _lib.tandem_attention, cfg, q.data_ptr(), k.data_ptr(), v.data_ptr(), offsets.data_ptr(), out.data_ptr(),
+         lse.data_ptr())
     return dict(out=out, lse=lse)
 
 
@@ -424,23 +463,28 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
     (tandem_attention_backward).  dq, dk, dv may be given, also as views (the
     value columns of qk_norm_rope_backward's dqkv).  Returns dq, dk, dv."""
     who = "attention_backward"
-    cfg = _attention_cfg(who, q, k, v, offsets, scale)
-    dev = q.device
-    cfg.out_stride = _rows(who, "out", out, q.dtype, q.shape, dev)
-    cfg.dout_stride = _rows(who, "dout", dout, q.dtype, q.shape, dev)
+    cfg, dt, dev = _attention_cfg(who, q, k, v, offsets, scale)
+    qs, ks = q.shape, k.shape
+    cfg.out_stride = _rows(who, "out", out, dt, qs, dev)
+    cfg.dout_stride = _rows(who, "dout", dout, dt, qs, dev)
     _same(who, "lse", lse, torch.float32, (cfg.n_q_heads, cfg.rows), dev)
-    dq = torch.empty(q.shape, dtype=q.dtype, device=dev) if dq is None else dq
-    dk = torch.empty(k.shape, dtype=q.dtype, device=dev) if dk is None else dk
-    dv = torch.empty(k.shape, dtype=q.dtype, device=dev) if dv is None else dv
-    cfg.dq_stride = _rows(who, "dq", dq, q.dtype, q.shape, dev)
-    cfg.dk_stride = _rows(who, "dk", dk, q.dtype, k.shape, dev)
-    cfg.dv_stride = _rows(who, "dv", dv, q.dtype, k.shape, dev)
-    need = L.tandem_attention_workspace_size(cfg)
+    if dq is None:
+        dq = torch.empty(qs, dtype=dt, device=dev)
+    else:
+        cfg.dq_stride = _rows(who, "dq", dq, dt, qs, dev)
+    if dk is None:
+        dk = torch.empty(ks, dtype=dt, device=dev)
+    else:
+        cfg.dk_stride = _rows(who, "dk", dk, dt, ks, dev)
+    if dv is None:
+        dv = torch.empty(ks, dtype=dt, device=dev)
+    else:
+        cfg.dv_stride = _rows(who, "dv", dv, dt, ks, dev)
+    need = _need(_lib.tandem_attention_workspace_size, cfg)
     workspace = _workspace(workspace, need, dev)
-    with torch.cuda.device(dev):
-        L.tandem_attention_backward(cfg, dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
-                                    lse.data_ptr(), offsets.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
-                                    _ptr(workspace), need, _on(dev))
+    _run(dev, _lib.tandem_attention_backward, cfg, dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+         out.data_ptr(), lse.data_ptr(), offsets.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+         _ptr(workspace), need)
     return dict(dq=dq, dk=dk, dv=dv)
 
 
@@ -463,10 +507,8 @@ class AdamW:
         if not self.params:
             raise ValueError("AdamW: no tensors")
         self.dev = self.params[0].device
-        _on(self.dev)
-        for p in self.params:
-            if p.dtype not in _DT or p.device != self.dev or not p.is_contiguous():
-                raise ValueError(f"AdamW: weights must be contiguous bfloat16 or float32 tensors on {self.dev}")
+        _gpu(self.dev)
+        self._check_params()
         n = len(self.params)
         decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * n
         if len(decay) != n:
@@ -492,9 +534,21 @@ class AdamW:
             if master:
                 for p, o in zip(self.params, self.offsets):
                     self.master[o:o + p.numel()].copy_(p.reshape(-1))
+        self._shapes = [p.shape for p in self.params]
+        self._types = [p.dtype for p in self.params]
+        # the tensors' table as the library reads it, and a view of it by columns
         self._table = (L.AdamwTensor * n)(*[
             L.AdamwTensor(p.data_ptr(), None, p.numel(), o, float(w), _DT[p.dtype], _DT[p.dtype])
             for p, o, w in zip(self.params, self.offsets, decay)])
+        self._columns = np.frombuffer(self._table, dtype=np.dtype(
+            [(name, {C.c_void_p: np.uint64, C.c_int64: np.int64, C.c_double: np.float64, C.c_int32: np.int32}[t])
+             for name, t in L.AdamwTensor._fields_]))
+        self._grad_types = self._types
+
+    def _check_params(self) -> None:
+        for p in self.params:
+            if p.dtype not in _DT or p.device != self.dev or not p.is_contiguous():
+                raise ValueError(f"AdamW: weights must be contiguous bfloat16 or float32 tensors on {self.dev}")
 
     def state(self) -> dict:
         """The optimizer's state, to be saved and given to another AdamW."""
@@ -505,21 +559,30 @@ class AdamW:
         float32).  Returns the gradients' norm before clipping, a float32 scalar on
         the device (None without clipping).  A step captured into a graph
         repeats that step's number when it is replayed."""
-        if len(grads) != len(self.params):
-            raise ValueError(f"AdamW: {len(grads)} gradients for {len(self.params)} tensors")
-        for d, g, p in zip(self._table, grads, self.params):
-            if g.shape != p.shape or g.dtype not in _DT or g.device != self.dev or not g.is_contiguous():
-                raise ValueError(f"AdamW: a gradient must be a contiguous bfloat16 or float32 tensor of shape "
-                                 f"{tuple(p.shape)} on {self.dev}")
-            # a weight whose storage was replaced since the last step is followed
-            d.param, d.grad, d.grad_dtype = p.data_ptr(), g.data_ptr(), _DT[g.dtype]
-        cfg = L.AdamwCfg(float(lr), float(self.betas[0]), float(self.betas[1]), self.eps, self.max_norm,
-                         self.steps + 1, self.elems)
-        need = L.tandem_adamw_workspace_size(cfg, self._table, len(self.params))
-        norm = torch.empty((), dtype=torch.float32, device=self.dev) if self.max_norm > 0 else None
+        index = self.dev.index
+        types = [g.dtype for g in grads]
+        if ([g.shape for g in grads] != self._shapes or not all([g.is_contiguous() for g in grads])
+                or [g.get_device() for g in grads] != [index] * len(self._shapes)):
+            raise ValueError(f"AdamW: the gradients must be contiguous tensors of the {len(self.params)} weights' shapes "
+                             f"on {self.dev}")
+        if types != self._grad_types:
+            if not all(t in _DT for t in types):
+                raise ValueError("AdamW: gradients must be bfloat16 or float32")
+            self._columns["grad_dtype"] = [_DT[t] for t in types]
+            self._grad_types = types
+        # a weight whose storage was replaced since the last step is followed
+        if [p.dtype for p in self.params] != self._types or [p.shape for p in self.params] != self._shapes:
+            raise ValueError("AdamW: a weight's type or shape has changed")
+        self._columns["param"] = [p.data_ptr() for p in self.params]
+        self._columns["grad"] = [g.data_ptr() for g in grads]
+        b1, b2 = self.betas
+        cfg = L.AdamwCfg(lr, b1, b2, self.eps, self.max_norm, self.steps + 1, self.elems)
+        need, norm = 0, None
+        if self.max_norm > 0:
+            need = _need(_lib.tandem_adamw_workspace_size, cfg, self._table, len(types))
+            norm = torch.empty((), dtype=torch.float32, device=self.dev)
         workspace = _workspace(None, need, self.dev)
-        with torch.cuda.device(self.dev):
-            L.tandem_adamw(cfg, self._table, len(self.params), self.m.data_ptr(), self.v.data_ptr(),
-                           _ptr(self.master), _ptr(norm), _ptr(workspace), need, _on(self.dev))
+        _run(self.dev, _lib.tandem_adamw, cfg, self._table, len(types), self.m.data_ptr(), self.v.data_ptr(),
+             _ptr(self.master), _ptr(norm), _ptr(workspace), need)
         self.steps += 1
         return norm
