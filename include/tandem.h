@@ -341,6 +341,8 @@ typedef struct {
   float eos_bias, eos_bias_ref;
 } tandem_logprob_cfg;
 
+/* Workspace of the forward pass: where few rows are cut into parts (0 otherwise;
+ * the workspace may then be NULL). */
 tandem_status tandem_logprob_workspace_size(const tandem_logprob_cfg* cfg, size_t* bytes);
 
 /* logits [R][V]; logits_ref [R][V] or NULL (no reference: kl and lse_diff

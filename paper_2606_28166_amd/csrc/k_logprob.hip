@@ -1,13 +1,14 @@
 // k_logprob.hip — log-probs of given tokens from logits, the divergence from a
 // reference model's logits, and the gradient of both with respect to the logits.
 //
-// Forward: one pass over a row with the running maximum m and the sums taken
-// against it, l = sum e^(s - m) and (with a reference) w = sum e^(s - m) (s - s'),
-// beside the reference's own m', l'.  Then lse = m + log l, logp = (s_y - m) - log l,
-// lse - lse' = (m - m') + log(l / l') and KL = w / l - (lse - lse'): each difference
-// is formed before it is added to something large, so a small KL keeps its digits.
+// Forward: one pass over a row with the running maximum m and the sums taken against
+// it, l = sum e^(s - m) and (with a reference) w = sum e^(s - m) (s - s'), beside the
+// reference's own m', l'.  Then lse = m + log l, logp = (s_y - m) - log l,
+// lse - lse' = (m - m') + log l - log l' and KL = w / l - (lse - lse').  The maxima are kept
+// in powers of two, rounded once, and everything is taken against the rounded numbers; the
+// differences are formed in 64 bits, once a row, so that a small KL keeps its digits.
 // Backward: p = e^(s - lse) again, elementwise.
-// All sums are float32, logits are converted as they are read.
+// The sums are float32, logits are converted as they are read.
 #include "common.h"
 #include "update.h"
 
@@ -19,7 +20,6 @@ typedef uint32_t u32x4_e2 __attribute__((ext_vector_type(4), aligned(2)));
 typedef float f32x4_e4 __attribute__((ext_vector_type(4), aligned(4)));
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
 
 // bf16 pair: element 0 in the low half
 __device__ __forceinline__ float lo16(uint32_t w) { return __uint_as_float(w << 16); }
@@ -57,88 +57,186 @@ __device__ __forceinline__ void store8(float* p, const float* v) {
 __device__ __forceinline__ void store1(bf16_t* p, float v) { *p = (bf16_t)bf16_any(v); }
 __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 
-// Statistics of a part of a row; m is in units of the (biased) logits.
+// Statistics of a part of a row; the maxima in powers of two.
 struct Stats {
   float m, l, w, mr, lr;
 };
+__device__ __forceinline__ Stats no_stats() { return Stats{-INFINITY, 0.f, 0.f, -INFINITY, 0.f}; }
 
-// What e^((z - m) / T) is taken against: a part with nothing above -inf has m =
-// -inf, and its differences must still be -inf and not NaN.
+// What a score is taken against: a part with nothing above -inf has m = -inf, and its
+// differences must still be -inf and not NaN.
 __device__ __forceinline__ float against(float m) { return m == -INFINITY ? 0.f : m; }
 
 template <bool REF>
-__device__ __forceinline__ Stats merge(const Stats& a, const Stats& b, float c2) {
+__device__ __forceinline__ Stats merge(const Stats& a, const Stats& b) {
   Stats r;
   r.m = fmaxf(a.m, b.m);
   const float m = against(r.m);
-  const float fa = __builtin_amdgcn_exp2f((a.m - m) * c2), fb = __builtin_amdgcn_exp2f((b.m - m) * c2);
+  const float fa = __builtin_amdgcn_exp2f(a.m - m), fb = __builtin_amdgcn_exp2f(b.m - m);
   r.l = a.l * fa + b.l * fb;
   r.w = r.mr = r.lr = 0.f;
   if (REF) {
     r.w = a.w * fa + b.w * fb;
     r.mr = fmaxf(a.mr, b.mr);
     const float n = against(r.mr);
-    r.lr = a.lr * __builtin_amdgcn_exp2f((a.mr - n) * c2) + b.lr * __builtin_amdgcn_exp2f((b.mr - n) * c2);
+    r.lr = a.lr * __builtin_amdgcn_exp2f(a.mr - n) + b.lr * __builtin_amdgcn_exp2f(b.mr - n);
   }
   return r;
 }
 
 template <bool REF>
-__device__ __forceinline__ Stats shuffle_merge(Stats s, int lanes, float c2) {
-  for (int o = lanes / 2; o > 0; o >>= 1) {
-    Stats t;
+__device__ __forceinline__ Stats wave_merge(Stats s) {
+#pragma unroll
+  for (int o = kWave / 2; o > 0; o >>= 1) {
+    Stats t = no_stats();
     t.m = __shfl_xor(s.m, o, kWave);
     t.l = __shfl_xor(s.l, o, kWave);
-    t.w = REF ? __shfl_xor(s.w, o, kWave) : 0.f;
-    t.mr = REF ? __shfl_xor(s.mr, o, kWave) : -INFINITY;
-    t.lr = REF ? __shfl_xor(s.lr, o, kWave) : 0.f;
-    s = merge<REF>(s, t, c2);
+    if (REF) {
+      t.w = __shfl_xor(s.w, o, kWave);
+      t.mr = __shfl_xor(s.mr, o, kWave);
+      t.lr = __shfl_xor(s.lr, o, kWave);
+    }
+    s = merge<REF>(s, t);
   }
   return s;
 }
 
-// Folds 8 entries (those past the row's end are -inf) into the running statistics.
-template <bool REF>
-__device__ __forceinline__ void fold8(Stats& s, const float* x, const float* y, float c2) {
-  float mx = s.m, my = s.mr;
+// 8 entries of a row and of the reference's.
+template <bool REF> struct Eight {
+  float x[8], y[8];
+
+  template <typename T> __device__ __forceinline__ void take(const Row8<T>& c, const Row8<T>& d) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    mx = fmaxf(mx, x[e]);
-    if (REF) my = fmaxf(my, y[e]);
+    for (int e = 0; e < 8; ++e) {
+      x[e] = c.get(e);
+      y[e] = REF ? d.get(e) : 0.f;
+    }
   }
-  const float m = against(mx), n = against(my);
-  const float f = __builtin_amdgcn_exp2f((s.m - m) * c2);
+  // entries v .. v1 - 1 of fewer than 8; -inf for the others
+  template <typename T> __device__ __forceinline__ void some(const T* z, const T* zr, int v, int v1) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      x[e] = v + e < v1 ? ld(z + v + e) : -INFINITY;
+      y[e] = REF && v + e < v1 ? ld(zr + v + e) : -INFINITY;
+    }
+  }
+  // a, b added to entry i where it is one of these
+  __device__ __forceinline__ void add(int i, float a, float b) {
+    if ((unsigned)i >= 8u) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      x[e] += e == i ? a : 0.f;
+      if (REF) y[e] += e == i ? b : 0.f;
+    }
+  }
+};
+
+// Folds 8 entries into the running statistics: some 13 vector operations per pair of
+// logits, an exponential counting two.
+template <bool REF>
+__device__ __forceinline__ void fold(Stats& s, const Eight<REF>& a, float c2) {
+  float mx = a.x[0], my = a.y[0], lo = fminf(a.x[0], a.y[0]);
+#pragma unroll
+  for (int e = 1; e < 8; ++e) {
+    mx = fmaxf(mx, a.x[e]);
+    if (REF) {
+      my = fmaxf(my, a.y[e]);
+      lo = fminf(lo, fminf(a.x[e], a.y[e]));
+    }
+  }
+  mx *= c2;
+  my *= c2;
+  if (__any(mx > s.m || (REF && my > s.mr))) {             // seldom, but at a row's beginning
+    const float m = fmaxf(s.m, mx), f = __builtin_amdgcn_exp2f(s.m - against(m));
+    s.l *= f;
+    s.m = m;
+    if (REF) {
+      const float n = fmaxf(s.mr, my);
+      s.w *= f;
+      s.lr *= __builtin_amdgcn_exp2f(s.mr - against(n));
+      s.mr = n;
+    }
+  }
+  const float m = -against(s.m), n = -against(s.mr);
+  // scores of -inf on either side: an entry of probability 0 adds nothing, whatever they differ by
+  const bool holes = REF && __any(lo == -INFINITY);
   float l = 0.f, w = 0.f, lr = 0.f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float p = __builtin_amdgcn_exp2f((x[e] - m) * c2);
+    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(a.x[e], c2, m));
     l += p;
     if (REF) {
-      w += p * (p > 0.f ? x[e] - y[e] : 0.f);
-      lr += __builtin_amdgcn_exp2f((y[e] - n) * c2);
+      if (!holes) w += p * (a.x[e] - a.y[e]);
+      else w += p > 0.f ? p * (a.x[e] - a.y[e]) : p;
+      lr += __builtin_amdgcn_exp2f(__builtin_fmaf(a.y[e], c2, n));
     }
   }
-  s.l = s.l * f + l;
-  s.m = mx;
+  s.l += l;
   if (REF) {
-    s.w = s.w * f + w;
-    s.lr = s.lr * __builtin_amdgcn_exp2f((s.mr - n) * c2) + lr;
-    s.mr = my;
+    s.w += w;
+    s.lr += lr;
   }
 }
 
-// A row's outputs from its statistics.
+// A row whose largest score is too low for powers of two, or that has none above -inf (the
+// senior's or the reference's): in units of the logits, by one wave.
 template <typename T, bool REF>
-__device__ __forceinline__ void finish(const LogprobArgs& a, int r, const Stats& s) {
+__device__ __forceinline__ void low_row(const LogprobArgs& a, int r, int lane) {
+  const T* z = reinterpret_cast<const T*>(a.z) + (size_t)r * a.ldz;
+  const T* zr = REF ? reinterpret_cast<const T*>(a.zr) + (size_t)r * a.ldr : nullptr;
+  auto at = [&](const T* p, int v, float b) { return ld(p + v) + (v == a.eos ? b : 0.f); };
+  float m = -INFINITY, n = -INFINITY;
+  for (int v = lane; v < a.V; v += kWave) {
+    m = fmaxf(m, at(z, v, a.bias));
+    if (REF) n = fmaxf(n, at(zr, v, a.bias_r));
+  }
+  m = wave_max(m);
+  n = wave_max(n);
+  double l = 0.0, w = 0.0, lr = 0.0;
+  for (int v = lane; v < a.V; v += kWave) {
+    const float x = at(z, v, a.bias), p = expf((x - against(m)) * a.inv_t);
+    l += (double)p;
+    if (REF) {
+      const float y = at(zr, v, a.bias_r);
+      w += p > 0.f ? (double)p * (double)(x - y) : (double)p;
+      lr += (double)expf((y - against(n)) * a.inv_t);
+    }
+  }
+#pragma unroll
+  for (int o = kWave / 2; o > 0; o >>= 1) {
+    l += __shfl_xor(l, o, kWave);
+    w += __shfl_xor(w, o, kWave);
+    lr += __shfl_xor(lr, o, kWave);
+  }
+  if (lane != 0) return;
+  const int y = a.tok[r];
+  const double t = (double)a.inv_t, ll = log(l);
+  a.logp[r] = (float)(((double)at(z, y, a.bias) - (double)m) * t - ll);
+  a.lse[r] = (float)((double)m * t + ll);
+  if (REF) {
+    const double diff = ((double)m - (double)n) * t + (ll - log(lr));
+    a.diff[r] = (float)diff;
+    a.kl[r] = (float)(w * t / l - diff);
+  }
+}
+
+// A row's outputs from its statistics, by one wave.
+template <typename T, bool REF>
+__device__ __forceinline__ void finish(const LogprobArgs& a, int r, const Stats& s, int lane) {
+  if (s.m < -1e30f || (REF && s.mr < -1e30f)) {
+    low_row<T, REF>(a, r, lane);
+    return;
+  }
+  if (lane != 0) return;
   const int y = a.tok[r];
   const float zy = ld(reinterpret_cast<const T*>(a.z) + (size_t)r * a.ldz + y) + (y == a.eos ? a.bias : 0.f);
-  const float ll = logf(s.l);
-  a.logp[r] = (zy - s.m) * a.inv_t - ll;
-  a.lse[r] = s.m * a.inv_t + ll;
+  const double ln2 = 0.69314718055994530942, ll = log2((double)s.l);
+  a.logp[r] = (float)((((double)zy * (double)(a.inv_t * kLog2e) - (double)s.m) - ll) * ln2);
+  a.lse[r] = (float)(((double)s.m + ll) * ln2);
   if (REF) {
-    const float diff = (s.m - s.mr) * a.inv_t + logf(s.l / s.lr);
-    a.diff[r] = diff;
-    a.kl[r] = s.w * a.inv_t / s.l - diff;
+    const double diff = (((double)s.m - (double)s.mr) + (ll - log2((double)s.lr))) * ln2;
+    a.diff[r] = (float)diff;
+    a.kl[r] = (float)((double)s.w * (double)a.inv_t / (double)s.l - diff);
   }
 }
 
@@ -148,79 +246,64 @@ __device__ __forceinline__ void left_out(const LogprobArgs& a, int r, bool ref) 
   if (ref) a.kl[r] = a.diff[r] = 0.f;
 }
 
-// NT threads per row part, 256 threads per workgroup.  gridDim.x covers the rows
-// (256 / NT per workgroup), gridDim.y the parts of a row.
+// NT threads per row: a wave, four rows to a workgroup, or a workgroup.  gridDim.x covers the
+// rows, gridDim.y the parts of a row.  A thread's next 8 entries are on their way while it
+// folds the last ones.
 template <typename T, bool REF, int NT>
 __global__ __launch_bounds__(256) void logprob_kernel(LogprobArgs a) {
   constexpr int RPB = 256 / NT;
   __shared__ Stats red[4];
-  const int tid = threadIdx.x % NT, r = blockIdx.x * RPB + threadIdx.x / NT;
-  const int part = blockIdx.y;
+  const int tid = threadIdx.x % NT, lane = threadIdx.x & 63, r = blockIdx.x * RPB + threadIdx.x / NT;
   // a row that is left out is uniform over its NT threads
   const int y = r < a.R ? a.tok[r] : -1;
   const bool live = y >= 0 && y < a.V;
-  if (NT == 256 && !live) {
-    if (part == 0 && tid == 0) left_out(a, r, REF);
+  if (!live) {
+    if (blockIdx.y == 0 && tid == 0 && r < a.R) left_out(a, r, REF);
     return;
   }
   const float c2 = a.inv_t * kLog2e;
-  Stats s = {-INFINITY, 0.f, 0.f, -INFINITY, 0.f};
-  if (live) {
-    const int v0 = part * a.chunk, v1 = min(a.V, v0 + a.chunk);
-    const T* z = reinterpret_cast<const T*>(a.z) + (size_t)r * a.ldz;
-    const T* zr = REF ? reinterpret_cast<const T*>(a.zr) + (size_t)r * a.ldr : nullptr;
-    auto biased = [&](float* x, float* q, int v) {
-      const int e0 = a.eos - v;
-      if (a.eos >= 0 && e0 >= 0 && e0 < 8) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (e == e0) {
-            x[e] += a.bias;
-            if (REF) q[e] += a.bias_r;
-          }
-      }
-    };
-    int v = v0 + 8 * tid;
-    for (; v + 8 <= v1; v += 8 * NT) {
-      Row8<T> c, d;
-      c.load(z + v);
-      if (REF) d.load(zr + v);
-      float x[8], q[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        x[e] = c.get(e);
-        q[e] = REF ? d.get(e) : 0.f;
-      }
-      biased(x, q, v);
-      fold8<REF>(s, x, q, c2);
-    }
-    if (v < v1) {
-      float x[8], q[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        x[e] = v + e < v1 ? ld(z + v + e) : -INFINITY;
-        q[e] = REF && v + e < v1 ? ld(zr + v + e) : -INFINITY;
-      }
-      biased(x, q, v);
-      fold8<REF>(s, x, q, c2);
-    }
+  Stats s = no_stats();
+  const int v0 = blockIdx.y * a.chunk, v1 = min(a.V, v0 + a.chunk);
+  const T* z = reinterpret_cast<const T*>(a.z) + (size_t)r * a.ldz;
+  const T* zr = REF ? reinterpret_cast<const T*>(a.zr) + (size_t)r * a.ldr : nullptr;
+  int v = v0 + 8 * tid;
+  Row8<T> c, d;
+  if (v + 8 <= v1) {
+    c.load(z + v);
+    if (REF) d.load(zr + v);
   }
-  s = shuffle_merge<REF>(s, NT < kWave ? NT : kWave, c2);
+  for (; v + 8 <= v1; v += 8 * NT) {
+    Eight<REF> e;
+    e.take(c, d);
+    if (v + 8 * NT + 8 <= v1) {
+      c.load(z + v + 8 * NT);
+      if (REF) d.load(zr + v + 8 * NT);
+    }
+    if (a.eos >= 0) e.add(a.eos - v, a.bias, a.bias_r);
+    fold<REF>(s, e, c2);
+  }
+  if (v < v1) {
+    Eight<REF> e;
+    e.some(z, zr, v, v1);
+    if (a.eos >= 0) e.add(a.eos - v, a.bias, a.bias_r);
+    fold<REF>(s, e, c2);
+  }
+  s = wave_merge<REF>(s);
   if (NT > kWave) {
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x / kWave] = s;
+    if (lane == 0) red[threadIdx.x / kWave] = s;
     __syncthreads();
+    if (threadIdx.x >= kWave) return;
     s = red[0];
 #pragma unroll
-    for (int i = 1; i < NT / kWave; ++i) s = merge<REF>(s, red[i], c2);
+    for (int i = 1; i < NT / kWave; ++i) s = merge<REF>(s, red[i]);
   }
-  if (tid != 0 || r >= a.R) return;
-  if (!live) {
-    left_out(a, r, REF);
-  } else if (a.splits > 1) {
-    float* p = a.part + ((size_t)r * a.splits + part) * kLogprobPart;
-    p[0] = s.m; p[1] = s.l; p[2] = s.w; p[3] = s.mr; p[4] = s.lr;
+  if (a.splits > 1) {
+    if (lane == 0) {
+      float* p = a.part + ((size_t)r * a.splits + blockIdx.y) * kLogprobPart;
+      p[0] = s.m; p[1] = s.l; p[2] = s.w; p[3] = s.mr; p[4] = s.lr;
+    }
   } else {
-    finish<T, REF>(a, r, s);
+    finish<T, REF>(a, r, s, lane);
   }
 }
 
@@ -230,18 +313,103 @@ __global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a) {
   const int r = blockIdx.x, lane = threadIdx.x;
   const int y = a.tok[r];
   if (y < 0 || y >= a.V) return;             // written by the first launch
-  const float c2 = a.inv_t * kLog2e;
-  Stats s = {-INFINITY, 0.f, 0.f, -INFINITY, 0.f};
+  Stats s = no_stats();
   for (int i = lane; i < a.splits; i += kWave) {
     const float* p = a.part + ((size_t)r * a.splits + i) * kLogprobPart;
-    s = merge<REF>(s, Stats{p[0], p[1], p[2], p[3], p[4]}, c2);
+    s = merge<REF>(s, Stats{p[0], p[1], p[2], p[3], p[4]});
   }
-  s = shuffle_merge<REF>(s, kWave, c2);
-  if (lane == 0) finish<T, REF>(a, r, s);
+  finish<T, REF>(a, r, wave_merge<REF>(s), lane);
 }
 
-// Elementwise over a part of a row: gridDim.x parts of kGradChunk entries, gridDim.y rows.
+// Elementwise over kGradChunk entries of a row.
 constexpr int kGradChunk = 8192;
+
+// What a row's gradient is made of: dz_v = p (A + B (z_v - z'_v)), and `at` more at the token.
+struct RowGrad {
+  float A, B, at, lse2, c2;
+};
+template <bool KL>
+__device__ __forceinline__ float grad_of(const RowGrad& g, float x, float y) {
+  const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x, g.c2, -g.lse2));
+  // an entry of probability 0 has no gradient, whatever the scores differ by
+  return KL ? (p > 0.f ? p * __builtin_fmaf(g.B, x - y, g.A) : p) : p * g.A;
+}
+
+template <typename T, bool KL>
+__device__ __forceinline__ void grad_chunk(const LogprobArgs& a, const RowGrad& g, const T* z, const T* zr, T* out,
+                                           int y, int v0, int v1) {
+  int v = v0 + 8 * (int)threadIdx.x;
+  constexpr int STEP = 8 * 256;
+  // two vectors of 8 at a time: both are on their way before the first is needed
+  for (; v + STEP + 8 <= v1; v += 2 * STEP) {
+    Row8<T> c[2], d[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      c[i].load(z + v + i * STEP);
+      if (KL) d[i].load(zr + v + i * STEP);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int u = v + i * STEP;
+      Eight<KL> e;
+      e.take(c[i], d[i]);
+      if (a.eos >= 0) e.add(a.eos - u, a.bias, a.bias_r);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) e.x[k] = grad_of<KL>(g, e.x[k], e.y[k]);
+      e.add(y - u, g.at, 0.f);
+      store8(out + u, e.x);
+    }
+  }
+  for (; v + 8 <= v1; v += STEP) {
+    Row8<T> c, d;
+    c.load(z + v);
+    if (KL) d.load(zr + v);
+    Eight<KL> e;
+    e.take(c, d);
+    if (a.eos >= 0) e.add(a.eos - v, a.bias, a.bias_r);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) e.x[k] = grad_of<KL>(g, e.x[k], e.y[k]);
+    e.add(y - v, g.at, 0.f);
+    store8(out + v, e.x);
+  }
+  for (; v < v1; ++v) {
+    const bool eos = v == a.eos;
+    const float x = ld(z + v) + (eos ? a.bias : 0.f), q = KL ? ld(zr + v) + (eos ? a.bias_r : 0.f) : 0.f;
+    store1(out + v, grad_of<KL>(g, x, q) + (v == y ? g.at : 0.f));
+  }
+}
+
+// The same where the log-sum-exp is too low to be told from the maximum (or there is none):
+// the row's maximum and sum anew, in units of the logits.  One workgroup takes the whole row:
+// the gradient may take the logits' place.
+template <typename T, bool REF>
+__device__ __forceinline__ void low_grad(const LogprobArgs& a, int r, int y, float g, float k, const T* z, const T* zr,
+                                         T* out) {
+  __shared__ float red[4];
+  __shared__ double sums[4];
+  auto at = [&](const T* p, int v, float b) { return ld(p + v) + (v == a.eos ? b : 0.f); };
+  float m = -INFINITY;
+  for (int v = threadIdx.x; v < a.V; v += 256) m = fmaxf(m, at(z, v, a.bias));
+  m = wave_max(m);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x / kWave] = m;
+  __syncthreads();
+  m = against(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
+  double l = 0.0;
+  for (int v = threadIdx.x; v < a.V; v += 256) l += (double)expf((at(z, v, a.bias) - m) * a.inv_t);
+#pragma unroll
+  for (int o = kWave / 2; o > 0; o >>= 1) l += __shfl_xor(l, o, kWave);
+  if ((threadIdx.x & 63) == 0) sums[threadIdx.x / kWave] = l;
+  __syncthreads();
+  l = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+  const bool kl = REF && k != 0.f;
+  const float shift = kl ? a.diff[r] + a.kl[r] : 0.f;
+  for (int v = threadIdx.x; v < a.V; v += 256) {
+    const float x = at(z, v, a.bias), p = (float)((double)expf((x - m) * a.inv_t) / l);
+    float d = g * ((v == y ? 1.f : 0.f) - p);
+    if (kl && !(p == 0.f)) d += k * p * ((x - at(zr, v, a.bias_r)) * a.inv_t - shift);
+    store1(out + v, d * a.inv_t);
+  }
+}
 
 template <typename T, bool REF>
 __global__ __launch_bounds__(256) void logprob_grad_kernel(LogprobArgs a, int parts) {
@@ -252,56 +420,25 @@ __global__ __launch_bounds__(256) void logprob_grad_kernel(LogprobArgs a, int pa
   const int v0 = part * kGradChunk, v1 = min(a.V, v0 + kGradChunk);
   T* out = reinterpret_cast<T*>(a.grad) + (size_t)r * a.ldg;
   if (g == 0.f && k == 0.f) {
-    const float zero[8] = {};
+    float zero[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) zero[e] = 0.f;
     int v = v0 + 8 * (int)threadIdx.x;
     for (; v + 8 <= v1; v += 2048) store8(out + v, zero);
     for (; v < v1; ++v) store1(out + v, 0.f);
     return;
   }
   const T* z = reinterpret_cast<const T*>(a.z) + (size_t)r * a.ldz;
-  const bool kl = REF && k != 0.f;           // uniform over the row
   const T* zr = REF ? reinterpret_cast<const T*>(a.zr) + (size_t)r * a.ldr : nullptr;
-  const float lse = a.lse[r];
-  // dz_v = p (A + B (z_v - z'_v)), and g / T more at the token
-  const float A = a.inv_t * (kl ? -g - k * (a.diff[r] + a.kl[r]) : -g);
-  const float B = kl ? a.inv_t * k * a.inv_t : 0.f;
-  const float at = g * a.inv_t;
-  auto one = [&](float x, float q) {
-    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x, a.inv_t, -lse) * kLog2e);
-    return REF ? p * (A + B * (kl && p > 0.f ? x - q : 0.f)) : p * A;
-  };
-  auto marked = [&](float* x, float* q, int v, int id, float b, float br) {
-    const int e0 = id - v;
-    if (e0 >= 0 && e0 < 8) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (e == e0) {
-          x[e] += b;
-          if (REF) q[e] += br;
-        }
-    }
-  };
-  int v = v0 + 8 * (int)threadIdx.x;
-  for (; v + 8 <= v1; v += 2048) {
-    Row8<T> c, d;
-    c.load(z + v);
-    if (kl) d.load(zr + v);
-    float x[8], q[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      x[e] = c.get(e);
-      q[e] = kl ? d.get(e) : 0.f;
-    }
-    if (a.eos >= 0) marked(x, q, v, a.eos, a.bias, a.bias_r);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = one(x[e], q[e]);
-    marked(x, q, v, y, at, 0.f);
-    store8(out + v, x);
-  }
-  for (; v < v1; ++v) {
-    const float b = v == a.eos ? a.bias : 0.f, br = v == a.eos ? a.bias_r : 0.f;
-    const float x = ld(z + v) + b, q = kl ? ld(zr + v) + br : 0.f;
-    store1(out + v, one(x, q) + (v == y ? at : 0.f));
+  const float at = g * a.inv_t, lse2 = a.lse[r] * kLog2e, c2 = a.inv_t * kLog2e;
+  if (!(lse2 > -1e30f)) {
+    if (part == 0) low_grad<T, REF>(a, r, y, g, k, z, zr, out);
+  } else if (REF && k != 0.f) {
+    const RowGrad q = {a.inv_t * (-g - k * (a.diff[r] + a.kl[r])), a.inv_t * k * a.inv_t, at, lse2, c2};
+    grad_chunk<T, true>(a, q, z, zr, out, y, v0, v1);
+  } else {
+    const RowGrad q = {-at, 0.f, at, lse2, c2};
+    grad_chunk<T, false>(a, q, z, nullptr, out, y, v0, v1);
   }
 }
 
@@ -312,7 +449,7 @@ hipError_t run(const LogprobArgs& a, hipStream_t st) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     logprob_join_kernel<T, REF><<<a.R, 64, 0, st>>>(a);
-  } else if (a.V <= 2048) {
+  } else if (a.V <= 2048) {                  // a short row is a wave's
     logprob_kernel<T, REF, 64><<<(a.R + 3) / 4, 256, 0, st>>>(a);
   } else {
     logprob_kernel<T, REF, 256><<<a.R, 256, 0, st>>>(a);
@@ -330,12 +467,16 @@ hipError_t run_grad(const LogprobArgs& a, hipStream_t st) {
 }  // namespace
 
 int logprob_splits(int R, int V, int* chunk) {
-  // Enough workgroups to fill the device (1024 of 256 threads), in parts of at
-  // least 4096 entries.
-  const int most = (V + 4095) / 4096;
+  // Few rows are cut into parts of at least 8192 entries, about 1024 workgroups together: one
+  // compute unit alone reads at some 46 GB/s (four rows of 151936 float32 logits and their
+  // reference, whole: 26 us by 1024 threads each; in parts 5 us, and 3 for the join).
+  const int most = V / 8192;
   int want = (1024 + R - 1) / (R > 0 ? R : 1);
   if (want > most) want = most;
-  if (want < 1) want = 1;
+  if (want < 2) {
+    *chunk = V;
+    return 1;
+  }
   int c = (V + want - 1) / want;
   c = (c + 2047) / 2048 * 2048;              // whole passes of 256 threads by 8 entries
   *chunk = c;

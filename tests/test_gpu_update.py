@@ -129,7 +129,7 @@ def _logprob_check(z, zr, tok, gl, gk, T, eos, b, br, call_fwd, call_bwd, dt):
 @pytest.mark.parametrize("R,V", [(1, 1), (3, 2), (5, 7), (1, 8), (9, 63), (2, 2047), (7, 2048), (3, 2049), (1, 4097),
                                  (2, 32001), (1, 151936), (1030, 513), (1100, 5003)])
 def test_logprob(R, V, dt):
-    """Rows in a wave, in a workgroup, cut into parts; odd lengths; with reference,
+    """Rows of a wave, of a workgroup, cut into parts; odd lengths; with reference,
     temperature and EOS biases; rows left out (token -1 or past the vocabulary)."""
     from paper_2606_28166_amd import engine as E
     _say("logprob", R, V, dt)
@@ -192,7 +192,17 @@ def test_logprob_masked_entries(dt, V):
     assert float(r["kl"][0]) == math.inf and math.isfinite(float(r["kl"][1]))
     g = E.token_logprob_backward(z, tok, r, gl, g_kl=gk, ref=zr)
     assert torch.equal(g, E.token_logprob_backward(z, tok, r, gl))
+    # a row of nothing but the lowest value is uniform, its gradient too, also in the logits' place
+    z, zr, tok, gl, gk = _logprob_inputs(3, V, dt, V + 2)
+    z[1] = low
+    tok.fill_(2)
+    r = E.token_logprob(z, tok)
+    assert abs(float(r["logp"][1]) + math.log(V)) <= 4 * U * math.log(V)
+    want = float(gl[1]) * (torch.nn.functional.one_hot(torch.tensor(2), V).to(DEV).to(F64) - 1.0 / V)
+    for out in (None, z):
+        _within(E.token_logprob_backward(z, tok, r, gl, out=out)[1], want, (_half(dt) + 8 * U) * want.abs(), "grad")
     # rows without a distribution
+    z, zr, tok, gl, gk = _logprob_inputs(2, V, dt, V + 1)
     z[0] = -math.inf
     z[1, 1] = math.nan
     r = E.token_logprob(z, tok)
