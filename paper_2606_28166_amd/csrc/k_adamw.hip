@@ -105,6 +105,7 @@ __global__ __launch_bounds__(1024) void adamw_clip_kernel(const double* part, in
                                                           float* norm, float* clip) {
   __shared__ double red[1024 / kWave];
   double sum = 0.0;
+#pragma unroll 8
   for (int i = threadIdx.x; i < chunks; i += 1024) sum += part[i];
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, kWave);

@@ -78,22 +78,29 @@ __global__ __launch_bounds__(256) void qk_kernel(QkArgs a, int phases) {
   const Place w = place<HD>(phases, blockIdx.x);
   if (w.row >= a.N) return;                  // LANES lanes of a head stay together
   const int i0 = 8 * w.lane;
+  const T* src = reinterpret_cast<const T*>(a.qkv) + (size_t)w.row * a.ld;
+  Vec8<T> u, v;
+  if (w.head < a.nq + a.nkv) {
+    u.load(src + w.head * HD + i0);
+    v.load(src + w.head * HD + H + i0);
+  }
   const double pos = (double)a.pos[w.row];
   float c[8], s[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) turn(pos * a.turns[i0 + e], &c[e], &s[e]);
-  const T* src = reinterpret_cast<const T*>(a.qkv) + (size_t)w.row * a.ld;
   T* q = reinterpret_cast<T*>(a.q) + (size_t)w.row * a.ldq;
   T* k = reinterpret_cast<T*>(a.k) + (size_t)w.row * a.ldk;
-  for (int h = w.head; h < a.nq + a.nkv; h += w.step) {
-    Vec8<T> u, v;
-    u.load(src + h * HD + i0);
-    v.load(src + h * HD + H + i0);
+  const int heads = a.nq + a.nkv;
+  for (int h = w.head; h < heads; h += w.step) {
     float x[8], y[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       x[e] = u.get(e);
       y[e] = v.get(e);
+    }
+    if (h + w.step < heads) {                // the next head's, on their way meanwhile
+      u.load(src + (h + w.step) * HD + i0);
+      v.load(src + (h + w.step) * HD + H + i0);
     }
     if (a.gq) {
       float q2 = 0.f;
@@ -129,31 +136,38 @@ __global__ __launch_bounds__(256) void qk_backward_kernel(QkArgs a, int phases) 
   for (int block = blockIdx.x; block * rows < a.N; block += gridDim.x) {
     const Place w = place<HD>(phases, block);
     if (w.row >= a.N) break;
-    const int i0 = 8 * w.lane;
-    const double pos = (double)a.pos[w.row];
-    float c[8], s[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) turn(pos * a.turns[i0 + e], &c[e], &s[e]);
+    const int i0 = 8 * w.lane, heads = a.nq + a.nkv;
     const T* src = reinterpret_cast<const T*>(a.qkv) + (size_t)w.row * a.ld;
     T* dst = reinterpret_cast<T*>(a.dqkv) + (size_t)w.row * a.ld;
     const T* dq = reinterpret_cast<const T*>(a.dq) + (size_t)w.row * a.ldq;
     const T* dk = reinterpret_cast<const T*>(a.dk) + (size_t)w.row * a.ldk;
-    for (int h = w.head; h < a.nq + a.nkv; h += w.step) {
+    Vec8<T> du, dv, xu, xv;                  // of the head at hand, then of the next one
+    auto load = [&](int h) {
+      const T* dy = h < a.nq ? dq + h * HD : dk + (h - a.nq) * HD;
+      du.load(dy + i0);
+      dv.load(dy + H + i0);
+      if (a.gq) {
+        xu.load(src + h * HD + i0);
+        xv.load(src + h * HD + H + i0);
+      }
+    };
+    if (w.head < heads) load(w.head);
+    const double pos = (double)a.pos[w.row];
+    float c[8], s[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) turn(pos * a.turns[i0 + e], &c[e], &s[e]);
+    for (int h = w.head; h < heads; h += w.step) {
       const bool is_q = h < a.nq;
-      const T* dy = is_q ? dq + h * HD : dk + (h - a.nq) * HD;
-      Vec8<T> u, v;
-      u.load(dy + i0);
-      v.load(dy + H + i0);
+      const Vec8<T> u = xu, v = xv;
       float t[8], b[8];                      // the rotation undone: dn
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float p = u.get(e), q = v.get(e);
+        const float p = du.get(e), q = dv.get(e);
         t[e] = p * c[e] + q * s[e];
         b[e] = q * c[e] - p * s[e];
       }
+      if (h + w.step < heads) load(h + w.step);
       if (a.gq) {
-        u.load(src + h * HD + i0);
-        v.load(src + h * HD + H + i0);
         float q2 = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) q2 += u.get(e) * u.get(e) + v.get(e) * v.get(e);
@@ -198,46 +212,57 @@ __global__ __launch_bounds__(256) void qk_backward_kernel(QkArgs a, int phases) 
   }
 }
 
-// The workgroups' sums, a wave per gain entry.
-__global__ __launch_bounds__(64) void qk_gain_kernel(const float* part, int blocks, int hd, float* dgq, float* dgk) {
-  const int i = blockIdx.x;
+// The workgroups' sums: 8 entries per workgroup, 32 threads each.
+__global__ __launch_bounds__(256) void qk_gain_kernel(const float* part, int blocks, int hd, float* dgq, float* dgk) {
+  __shared__ double red[32][8];
+  const int e = threadIdx.x & 7, g = threadIdx.x >> 3, i = 8 * blockIdx.x + e;
   double sum = 0.0;
-  for (int b = threadIdx.x; b < blocks; b += kWave) sum += (double)part[(size_t)b * 2 * hd + i];
+#pragma unroll 8
+  for (int b = g; b < blocks; b += 32) sum += (double)part[(size_t)b * 2 * hd + i];
+  red[g][e] = sum;
+  __syncthreads();
+  if (g != 0) return;
+  sum = 0.0;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, kWave);
-  if (threadIdx.x == 0) (i < hd ? dgq[i] : dgk[i - hd]) = (float)sum;
+  for (int j = 0; j < 32; ++j) sum += red[j][e];
+  (i < hd ? dgq[i] : dgk[i - hd]) = (float)sum;
 }
 
-// Heads of a row side by side: a power of two that leaves each lane about four heads
-// for its angles, within one wave.
-int head_phases(int nq, int nkv, int hd) {
+// Heads of a row side by side: a power of two that leaves each lane about four heads for
+// its angles, more of them where the rows alone would not give the device four workgroups
+// per compute unit.  4097 rows of 24 heads of 128, backward: 26 us with 4 side by side, 21
+// with 8, 24 with 16.
+int head_phases(int N, int nq, int nkv, int hd) {
+  const int lanes = hd / 16;
   int p = 1;
-  while (2 * p * (hd / 16) <= kWave && 8 * p <= nq + nkv) p *= 2;
+  while (2 * p * lanes <= 256 && p < nq + nkv &&
+         (8 * p <= nq + nkv ? 2 * p * lanes <= kWave : (int64_t)N * p * lanes < 1024 * 256))
+    p *= 2;
   return p;
 }
 
 template <typename T, int HD>
 hipError_t run(const QkArgs& a, hipStream_t st) {
-  const int ph = head_phases(a.nq, a.nkv, HD), rows = 256 / (HD / 16) / ph;
+  const int ph = head_phases(a.N, a.nq, a.nkv, HD), rows = 256 / (HD / 16) / ph;
   qk_kernel<T, HD><<<(a.N + rows - 1) / rows, 256, 0, st>>>(a, ph);
   return hipGetLastError();
 }
 template <typename T, int HD>
 hipError_t run_backward(const QkArgs& a, hipStream_t st) {
-  const int ph = head_phases(a.nq, a.nkv, HD), blocks = qk_backward_blocks(a.N, a.nq, a.nkv, HD);
+  const int ph = head_phases(a.N, a.nq, a.nkv, HD), blocks = qk_backward_blocks(a.N, a.nq, a.nkv, HD);
   qk_backward_kernel<T, HD><<<blocks, 256, 0, st>>>(a, ph);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.gq) return e;
-  qk_gain_kernel<<<2 * HD, 64, 0, st>>>(a.part, blocks, HD, a.dgq, a.dgk);
+  qk_gain_kernel<<<2 * HD / 8, 256, 0, st>>>(a.part, blocks, HD, a.dgq, a.dgk);
   return hipGetLastError();
 }
 
 }  // namespace
 
 int qk_backward_blocks(int N, int nq, int nkv, int hd) {
-  const int rows = 256 / (hd / 16) / head_phases(nq, nkv, hd);
+  const int rows = 256 / (hd / 16) / head_phases(N, nq, nkv, hd);
   const int most = N > 0 ? (N + rows - 1) / rows : 1;      // no rows: one workgroup writes sums of 0
-  return most < 2048 ? most : 2048;
+  return most < 1024 ? most : 1024;
 }
 
 #define TANDEM_QK_DISPATCH(fn)                                             \
