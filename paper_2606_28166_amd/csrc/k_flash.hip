@@ -50,6 +50,7 @@ template <int HD> struct Ops<bf16_t, HD> {
   static constexpr int CPR = HD / 8;                       // chunks per row
   static constexpr int ROW = HD * 2;                       // bytes per row
   static constexpr int WGS = 2;                            // workgroups per compute unit (registers)
+  static constexpr int FWD = HD == 128 ? 3 : 4;            // of the forward pass
   struct Right { bf16x8_t b[HD / 16]; };                   // 32 columns, summed over the head dimension
   struct Prob { bf16x8_t b[2]; };                          // 32 x 32, summed over its rows
   struct Lanes { int rows[HD / 16], cols[2][HD / 32]; };
@@ -81,25 +82,6 @@ template <int HD> struct Ops<bf16_t, HD> {
 #pragma unroll
     for (int i = 0; i < 16; ++i) r.b[i >> 3][i & 7] = (__bf16)p[i];
     return r;
-  }
-  // The order of a stretch of code with N products: a product, the reads (R) for a later one,
-  // and as much vector work (V operations, E exponentials) as its time on the matrix pipe
-  // hides.
-  template <int N, int R, int V, int E>
-  __device__ __forceinline__ static void interleave() {
-    __builtin_amdgcn_sched_group_barrier(0x100, 2 * R, 0);
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
-      __builtin_amdgcn_sched_group_barrier(0x002, V, 0);
-      __builtin_amdgcn_sched_group_barrier(0x400, E, 0);
-    }
-  }
-  // p by a power of two: exact, but for what falls below the type's range
-  __device__ __forceinline__ static void scale(Prob& p, float by) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) p.b[i >> 3][i & 7] = (__bf16)((float)p.b[i >> 3][i & 7] * by);
   }
   // this lane's part of the sum of a b over the head dimension
   __device__ __forceinline__ static float dot(const Right& a, const Right& b) {
@@ -142,6 +124,7 @@ template <int HD> struct Ops<float, HD> {
   static constexpr int CPR = HD / 4;
   static constexpr int ROW = HD * 4;
   static constexpr int WGS = HD == 128 ? 1 : 2;
+  static constexpr int FWD = HD == 128 ? 2 : HD == 64 ? 3 : 4;
   struct Right { float b[HD / 2]; };
   struct Prob { float b[16]; };
   struct Lanes { int rows[HD / 8], cols[2][4]; };
@@ -175,11 +158,6 @@ template <int HD> struct Ops<float, HD> {
 #pragma unroll
     for (int i = 0; i < 16; ++i) r.b[i] = p[i];
     return r;
-  }
-  template <int N, int R, int V, int E> __device__ __forceinline__ static void interleave() {}
-  __device__ __forceinline__ static void scale(Prob& p, float by) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) p.b[i] *= by;
   }
   __device__ __forceinline__ static float dot(const Right& a, const Right& b) {
     float s = 0.f;
@@ -216,7 +194,8 @@ template <int HD> struct Ops<float, HD> {
 // one for each of a wave's instructions within 16 rows.
 template <typename T, int HD, int ROWS = kRows, int WAVES = kWaves> struct Stager {
   using O = Ops<T, HD>;
-  static constexpr int COUNT = ROWS * O::CPR / (64 * WAVES);          // instructions of a wave
+  static constexpr int TOTAL = ROWS * O::CPR / 64;                    // instructions of a tile
+  static constexpr int COUNT = (TOTAL + WAVES - 1) / WAVES;           // of a wave, at most
   static constexpr int PASS = 64 * WAVES / O::CPR;                    // rows of one instruction of every wave
   static constexpr int KINDS = PASS < 16 ? 16 / PASS : 1;
   uint32_t at[KINDS], ld;        // bytes: this lane's chunks in memory; a row
@@ -235,7 +214,7 @@ template <typename T, int HD, int ROWS = kRows, int WAVES = kWaves> struct Stage
     const __amdgpu_buffer_rsrc_t r = buf_rsrc(g, bytes);
 #pragma unroll
     for (int j = 0; j < COUNT; ++j)
-      buf_load_lds16(r, tile + (wave + WAVES * j) * 1024, (int)(at[j % KINDS] + (j / KINDS) * KINDS * PASS * ld), 0);
+      if (TOTAL % WAVES == 0 || wave + WAVES * j < TOTAL) buf_load_lds16(r, tile + (wave + WAVES * j) * 1024, (int)(at[j % KINDS] + (j / KINDS) * KINDS * PASS * ld), 0);
   }
 };
 
@@ -349,23 +328,21 @@ __device__ __forceinline__ float other_max(float v) {
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-// The running softmax of a wave's 32 queries over blocks of 32 keys, in three stages that
-// overlap: while the matrix pipe forms block j + 1's scores and adds block j - 1's values,
-// the vector unit takes block j's exponentials.  m2 is the maximum (in powers of two, a
-// whole number) that the sums are taken against.  It is raised only where a score passes it
+// The running softmax of a wave's 32 queries over blocks of 32 keys.  m2 is the maximum (in
+// powers of two) that the sums are taken against; it is raised only where a score passes it
 // by 2^8, which float32 sums and bf16's range bear, so that most blocks leave the
-// accumulator alone; the probabilities on their way are then scaled exactly.
+// accumulator alone.
 template <typename T, int HD>
 struct Softmax {
   using O = Ops<T, HD>;
-  float m2, l;
+  float m2 = -INFINITY, l = 0.f;
   f32x16_t o[HD / 32];
-  f32x16_t s;                    // block j's scores
-  typename O::Prob p;            // block j - 1's probabilities
 
-  // A block's scores, its first key at n0, become block j.
-  __device__ __forceinline__ void take(const f32x16_t& next, int n0, int q0, int qi, float s2, int h) {
-    s = next;
+  // A block of keys, the first at n0.
+  __device__ __forceinline__ void add(const char* __restrict__ tk, const char* __restrict__ tv,
+                                      const typename O::Lanes& at, const typename O::Right& q, int n0, int q0, int qi,
+                                      float s2, int h) {
+    f32x16_t s = O::by_rows(tk, at, 0, q);
     if (n0 + 31 > q0) {
 #pragma unroll
       for (int i = 0; i < 16; ++i)
@@ -376,46 +353,33 @@ struct Softmax {
     for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
     mx = other_max(mx) * s2;
     if (__any(mx > m2 + 8.f)) {
-      const float m = fmaxf(m2, ceilf(mx)), f = __builtin_amdgcn_exp2f(m2 - m);
+      const float m = fmaxf(m2, mx), f = __builtin_amdgcn_exp2f(m2 - m);
       m2 = m;
       l *= f;
 #pragma unroll
       for (int d = 0; d < HD / 32; ++d) o[d] *= f;
-      O::scale(p, f);
     }
-  }
-  __device__ __forceinline__ typename O::Prob exponentials(float s2) {
-    float e[16];
+    float p[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], s2, -m2));
-      l += e[i];
+      p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], s2, -m2));
+      l += p[i];
     }
-    asm volatile("" : "+v"(l));    // the sum is made here, not where it is next used with 16 registers kept for it
-    return O::pack(e);
-  }
-  // Rows k0 .. of the keys' tile are block j + 1, rows v0 .. of the values' tile block j - 1.
-  __device__ __forceinline__ f32x16_t advance(const char* __restrict__ tk, int k0, const char* __restrict__ tv, int v0,
-                                              const typename O::Lanes& at, const typename O::Right& q, float s2) {
-    const f32x16_t next = O::by_rows(tk, at, k0, q);
-    O::transposed(o, tv, at, v0, p);
-    p = exponentials(s2);
-    O::template interleave<HD / 8, HD == 128 ? 2 : 2, 320 / HD + 1, 128 / HD>();
-    return next;
-  }
-  // The same at the end: no further scores.
-  __device__ __forceinline__ void drain(const char* __restrict__ tv, const typename O::Lanes& at, float s2) {
-    O::transposed(o, tv, at, 0, p);
-    p = exponentials(s2);
-    O::transposed(o, tv, at, 32, p);
+    O::transposed(o, tv, at, 0, O::pack(p));
   }
 };
 
+// Bound by latency more than by any one pipe: what counts is the waves a SIMD holds, so the
+// tiles are of 32 keys and the code keeps nothing ahead.  Heads of 128 take 161 registers,
+// three waves a SIMD: sixteen ragged rollouts (32 heads on 8) 279 us, 0.9 PFLOP/s.  Two waves with
+// tiles of 64 and the scores, exponentials and value products of three blocks
+// interleaved in each took 314, two without that 325.
 template <typename T, int HD>
-__global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_kernel(FlashArgs a) {
+__global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::FWD)) void flash_kernel(FlashArgs a) {
   using O = Ops<T, HD>;
-  constexpr int TILE = kRows * O::ROW;
+  constexpr int TILE = 32 * O::ROW;
   __shared__ __align__(16) char lds[2][2][TILE];           // [turn][keys, values]
+  static_assert(sizeof(lds) >= kWaves * 32 * O::ROW, "room for the results");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = lane >> 5, col = lane & 31;
   const int group = a.nq / a.nkv, together = heads_together(group), per = 32 * (kWaves / together);
@@ -428,54 +392,29 @@ __global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_kernel(F
   const int64_t row = w.start + min(qi, w.len - 1);
   const T* kb = reinterpret_cast<const T*>(a.k) + (int64_t)w.start * a.ldk + kv * HD;
   const T* vb = reinterpret_cast<const T*>(a.v) + (int64_t)w.start * a.ldv + kv * HD;
-  const Stager<T, HD> sk(a.ldk, lane, wave), sv(a.ldv, lane, wave);
-  const int end = min(w.len, w.first + per);               // keys that any row of the tile sees
-  const int tiles = (end + kRows - 1) / kRows;
-  const int mine = q0 < w.len ? q0 / kRows + 1 : 0;        // tiles that this wave's rows see
-  // keys run one tile ahead of values
-  const int64_t dk = (int64_t)kRows * a.ldk, dv = (int64_t)kRows * a.ldv;
-  auto load_k = [&](int i) {
-    sk.load(lds[i & 1][0], kb, w.len - i * kRows, wave);
+  const Stager<T, HD, 32> sk(a.ldk, lane, wave), sv(a.ldv, lane, wave);
+  const int tiles = (min(w.len, w.first + per) + 31) / 32;          // that any row of the workgroup sees
+  const int mine = q0 < w.len ? q0 / 32 + 1 : 0;                    // that this wave's rows see
+  const int64_t dk = 32 * a.ldk, dv = 32 * a.ldv;
+  auto load = [&](int t, int i) {
+    sk.load(lds[t][0], kb, w.len - 32 * i, wave);
+    sv.load(lds[t][1], vb, w.len - 32 * i, wave);
     kb += dk;
-  };
-  auto load_v = [&](int i) {
-    sv.load(lds[i & 1][1], vb, w.len - i * kRows, wave);
     vb += dv;
   };
-  load_k(0);
-  load_v(0);
-  if (tiles > 1) load_k(1);
+  load(0, 0);
   typename O::Right q;
   O::load_right(q, reinterpret_cast<const T*>(a.q) + row * a.ldq + head * HD, h);
   const float s2 = a.scale * kLog2e;
   const typename O::Lanes at = O::lanes(lane);
   Softmax<T, HD> st;
-  st.m2 = -INFINITY;
-  st.l = 0.f;
 #pragma unroll
   for (int d = 0; d < HD / 32; ++d) st.o[d] = zero16();
-  meet();
-  if (mine > 0) {
-    const float none[16] = {};
-    st.p = O::pack(none);
-    st.take(O::by_rows(lds[0][0], at, 0, q), 0, q0, qi, s2, h);
-    const f32x16_t second = O::by_rows(lds[0][0], at, 32, q);
-    st.p = st.exponentials(s2);
-    st.take(second, 32, q0, qi, s2, h);
-  }
-  // Step i: blocks 2 i and 2 i + 1's values (tile i), scores of tile i + 1.
   auto step = [&](auto turn, int i) {
     constexpr int t = decltype(turn)::value;
     meet();
-    if (i + 2 < tiles) load_k(i + 2);
-    if (i + 1 < tiles) load_v(i + 1);
-    if (i + 1 < mine) {
-      const int n0 = (i + 1) * kRows;
-      st.take(st.advance(lds[t ^ 1][0], 0, lds[t][1], 0, at, q, s2), n0, q0, qi, s2, h);
-      st.take(st.advance(lds[t ^ 1][0], 32, lds[t][1], 32, at, q, s2), n0 + 32, q0, qi, s2, h);
-    } else if (i < mine) {
-      st.drain(lds[t][1], at, s2);
-    }
+    if (i + 1 < tiles) load(t ^ 1, i + 1);
+    if (i < mine) st.add(lds[t][0], lds[t][1], at, q, 32 * i, q0, qi, s2, h);
   };
   for (int i = 0; i < tiles; i += 2) {
     step(Turn<0>{}, i);
