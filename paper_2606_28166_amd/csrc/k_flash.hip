@@ -659,27 +659,36 @@ __device__ __forceinline__ void store_column(float* p, const f32x16_t* acc, floa
 
 // dK and dV of bf16 heads of 64 and 128 by pairs of waves: of each pair's 32 keys one wave
 // forms the probabilities and dV, the other dP and dK.  Each then holds one operand and one
-// accumulator (of heads of 128 two waves fit a SIMD, where one wave with both has it alone; of 64 four), and while one
-// takes exponentials the other feeds the matrix pipe.  The probabilities go through LDS in
-// float32, lane to lane, and the second wave is one step of 32 queries behind the first, so
-// that a step has one meeting.  Four tiles are in LDS: behind, current, arrived, arriving.
+// accumulator (of heads of 128 two waves fit a SIMD, where one wave with both has it
+// alone), and while one takes exponentials the other feeds the matrix pipe.  The
+// probabilities go through LDS in float32, lane to lane (rounded to bf16 they would round
+// dS twice), and the second wave is one step of 32 queries behind the first, so that a step
+// has one meeting.  Three tiles are in LDS: behind, current, arriving.
+//
+// Bound by LDS: a pair reads 36 KB and writes 4 for its 32 products of a head of 128, which
+// is as much as a compute unit's LDS gives in the products' own time.  Two pairs to a
+// workgroup leave two workgroups on a compute unit that do not wait for each other:
+// sixteen ragged rollouts 649 us (four pairs and a deeper ring 645, six at three waves a SIMD 690), 200
+// sequences of at most 30 positions, backward as a whole, 68 us where four pairs take 90.
 //
 // Where the tiles of keys are few, a workgroup takes one part of the group's heads and
 // writes float32 sums, which flash_join_kernel adds up.
+constexpr int kPairs = 2;
+
 template <int HD>
-__global__ __launch_bounds__(512, (HD == 64 ? 4 : 2)) void flash_dkv_pair_kernel(FlashArgs a, int parts) {
+__global__ __launch_bounds__(128 * kPairs, (HD == 64 ? 3 : 2)) void flash_dkv_pair_kernel(FlashArgs a, int parts) {
   using O = Ops<bf16_t, HD>;
-  using S = Stager<bf16_t, HD, 32, 4>;
-  constexpr int TILE = 32 * O::ROW, LOADS = S::COUNT + 1;
-  __shared__ __align__(16) char lds[4][2][TILE];           // [turn][queries, output gradients]
-  __shared__ __align__(16) float prob[2][4][1024];         // [turn][pair]: probabilities in lane order
-  __shared__ __align__(16) float stat[4][8][64];           // [turn][wave]: log-sum-exps, negated deltas
+  using S = Stager<bf16_t, HD, 32, kPairs>;
+  constexpr int TILE = 32 * O::ROW, TURNS = 3;
+  __shared__ __align__(16) char lds[TURNS][2][TILE];       // [turn][queries, output gradients]
+  __shared__ __align__(16) float prob[2][kPairs][1024];     // [turn][pair]: probabilities in lane order
+  __shared__ __align__(16) float stat[TURNS][2 * kPairs][64];         // [turn][wave]: log-sum-exps, negated deltas
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int h = lane >> 5, col = lane & 31, pair = wave & 3;
-  const bool second = wave >= 4;
+  const bool second = wave >= kPairs;
+  const int h = lane >> 5, col = lane & 31, pair = second ? wave - kPairs : wave;
   const int kv = blockIdx.x % a.nkv, part = blockIdx.x / a.nkv % parts, slot = blockIdx.x / a.nkv / parts;
   const int group = a.nq / a.nkv / parts, head0 = kv * group * parts + part * group;
-  const Span w = find_span(a.offs, a.n_seqs, a.N, slot, 128, false);
+  const Span w = find_span(a.offs, a.n_seqs, a.N, slot, 32 * kPairs, false);
   if (w.first >= w.len) return;
   const int k0 = w.first + 32 * pair, ki = k0 + col;
   const int64_t row = w.start + min(ki, w.len - 1);
@@ -709,53 +718,41 @@ __global__ __launch_bounds__(512, (HD == 64 ? 4 : 2)) void flash_dkv_pair_kernel
       src_stat = head_stat += a.N;
     }
   };
-  load(0);
-  if (total > 1) load(1);
+  if (total > 0) load(0);
   const typename O::Lanes at = O::lanes(lane);
   const float s2 = a.scale * kLog2e;
   f32x16_t acc[HD / 32];
 #pragma unroll
   for (int d = 0; d < HD / 32; ++d) acc[d] = zero16();
-  // what a step begins with: its own tile has arrived everywhere, one more may be on its way
+  // what a step begins with: its tiles have arrived everywhere, the next ones are sent for
   auto begin = [&](int t, int i) {
-    if (i + 1 < total) meet<LOADS>();
-    else meet<0>();
-    if (i + 2 < total) load((t + 2) & 3);
+    meet();
+    if (i + 1 < total) load((t + 1) % TURNS);
   };
   int m0 = w.first;                                        // queries of the step at hand
   auto next = [&]() {
     m0 += 32;
     if (m0 >= w.len) m0 = w.first;
   };
-  auto first_step = [&](auto turn, int i) {
-    constexpr int t = decltype(turn)::value;
-    begin(t, i);
-    if (i >= total) return;
-    if (m0 >= k0)
-      dv_step<HD>(acc, lds[t][0], lds[t][1], stat[t][wave], prob[t & 1][pair], at, own, m0 == k0, col, s2, h, lane);
-    next();
-  };
-  auto second_step = [&](auto turn, int i) {
-    constexpr int t = decltype(turn)::value, b = (t + 3) & 3;      // the step before
-    begin(t, i);
-    if (i == 0) return;
-    if (m0 >= k0) dk_step<HD>(acc, lds[b][0], lds[b][1], stat[b][wave], prob[b & 1][pair], at, own, h, lane);
-    next();
-  };
-  // one step more than there are: the second wave's last
+  // One step more than there are: the second wave's last.
   if (second) {
-    for (int i = 0; i <= total; i += 4) {
-      second_step(Turn<0>{}, i);
-      if (i + 1 <= total) second_step(Turn<1>{}, i + 1);
-      if (i + 2 <= total) second_step(Turn<2>{}, i + 2);
-      if (i + 3 <= total) second_step(Turn<3>{}, i + 3);
+    for (int i = 0, t = 0, b = 0; i <= total; ++i) {
+      begin(t, i);
+      if (i > 0) {
+        if (m0 >= k0) dk_step<HD>(acc, lds[b][0], lds[b][1], stat[b][wave], prob[(i - 1) & 1][pair], at, own, h, lane);
+        next();
+      }
+      b = t;
+      t = t == TURNS - 1 ? 0 : t + 1;
     }
   } else {
-    for (int i = 0; i <= total; i += 4) {
-      first_step(Turn<0>{}, i);
-      if (i + 1 <= total) first_step(Turn<1>{}, i + 1);
-      if (i + 2 <= total) first_step(Turn<2>{}, i + 2);
-      if (i + 3 <= total) first_step(Turn<3>{}, i + 3);
+    for (int i = 0, t = 0; i <= total; ++i) {
+      begin(t, i);
+      if (i == total) break;
+      if (m0 >= k0)
+        dv_step<HD>(acc, lds[t][0], lds[t][1], stat[t][wave], prob[i & 1][pair], at, own, m0 == k0, col, s2, h, lane);
+      next();
+      t = t == TURNS - 1 ? 0 : t + 1;
     }
   }
   meet();                                                  // the tiles' room takes the results
@@ -811,7 +808,8 @@ hipError_t run_backward(const FlashArgs& a, hipStream_t st) {
   if (e != hipSuccess) return e;
   if constexpr (sizeof(T) == 2 && HD >= 64) {
     const int parts = flash_parts(a.N, a.n_seqs, a.nq, a.nkv, HD, DT_BF16);
-    flash_dkv_pair_kernel<HD><<<(unsigned)(slots_of(a, 128) * (int64_t)a.nkv * parts), 512, 0, st>>>(a, parts);
+    flash_dkv_pair_kernel<HD><<<(unsigned)(slots_of(a, 32 * kPairs) * (int64_t)a.nkv * parts), 128 * kPairs, 0, st>>>(
+        a, parts);
     if (parts > 1) {
       const hipError_t f = hipGetLastError();
       if (f != hipSuccess) return f;
@@ -826,12 +824,15 @@ hipError_t run_backward(const FlashArgs& a, hipStream_t st) {
 }  // namespace
 
 int flash_parts(int N, int n_seqs, int nq, int nkv, int hd, int dtype) {
-  // Tiles of keys differ in work by as much as a sequence is long, so it takes some three
-  // per compute unit to fill the device evenly.  With fewer, every head of the group is a
-  // part of its own: one sequence of 8703, 16 heads of 64 on 4, 769 us in 276 tiles, 362
-  // and 13 for the sums in 1104 parts.
-  const int64_t tiles = ((int64_t)N / 128 + n_seqs) * nkv;
-  return dtype == DT_BF16 && hd >= 64 && tiles < 768 ? nq / nkv : 1;
+  if (n_seqs < 1) return 1;
+  // Two workgroups of 64 keys fit a compute unit, and tiles differ in work by as much as their
+  // sequence is long.  Below half of the device, and of long sequences below two rounds of it, every
+  // head of the group is a part of its own: one sequence of 8703, 16 heads of 64 on 4, 769 us
+  // in tiles, 375 and 13 for the sums in parts.  Of short ones the sums cost more than the
+  // evenness gains: 64 sequences of at most 200, 32 heads of 128 on 8, 135 us whole, 258 in parts.
+  const int64_t tiles = ((int64_t)N / 64 + n_seqs / 2) * nkv;
+  const bool cut = tiles < 256 || (tiles < 1024 && N / n_seqs >= 1024);
+  return dtype == DT_BF16 && hd >= 64 && cut ? nq / nkv : 1;
 }
 
 #define TANDEM_FLASH_DISPATCH(fn)                                                            \
