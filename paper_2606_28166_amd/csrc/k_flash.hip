@@ -49,7 +49,7 @@ template <typename T, int HD> struct Ops;
 template <int HD> struct Ops<bf16_t, HD> {
   static constexpr int CPR = HD / 8;                       // chunks per row
   static constexpr int ROW = HD * 2;                       // bytes per row
-  static constexpr int WGS = 2;                            // workgroups per compute unit (registers)
+  static constexpr int WGS = 2;                            // workgroups per compute unit (registers): dQ
   static constexpr int FWD = HD == 128 ? 3 : 4;            // of the forward pass
   struct Right { bf16x8_t b[HD / 16]; };                   // 32 columns, summed over the head dimension
   struct Prob { bf16x8_t b[2]; };                          // 32 x 32, summed over its rows
@@ -214,7 +214,8 @@ template <typename T, int HD, int ROWS = kRows, int WAVES = kWaves> struct Stage
     const __amdgpu_buffer_rsrc_t r = buf_rsrc(g, bytes);
 #pragma unroll
     for (int j = 0; j < COUNT; ++j)
-      if (TOTAL % WAVES == 0 || wave + WAVES * j < TOTAL) buf_load_lds16(r, tile + (wave + WAVES * j) * 1024, (int)(at[j % KINDS] + (j / KINDS) * KINDS * PASS * ld), 0);
+      if (TOTAL % WAVES == 0 || wave + WAVES * j < TOTAL)
+        buf_load_lds16(r, tile + (wave + WAVES * j) * 1024, (int)(at[j % KINDS] + (j / KINDS) * KINDS * PASS * ld), 0);
   }
 };
 
@@ -659,17 +660,19 @@ __device__ __forceinline__ void store_column(float* p, const f32x16_t* acc, floa
 
 // dK and dV of bf16 heads of 64 and 128 by pairs of waves: of each pair's 32 keys one wave
 // forms the probabilities and dV, the other dP and dK.  Each then holds one operand and one
-// accumulator (of heads of 128 two waves fit a SIMD, where one wave with both has it
-// alone), and while one takes exponentials the other feeds the matrix pipe.  The
+// accumulator (of heads of 128 two waves fit a SIMD, of 64 three, where one wave with both
+// has it alone), and while one takes exponentials the other feeds the matrix pipe.  The
 // probabilities go through LDS in float32, lane to lane (rounded to bf16 they would round
 // dS twice), and the second wave is one step of 32 queries behind the first, so that a step
 // has one meeting.  Three tiles are in LDS: behind, current, arriving.
 //
 // Bound by LDS: a pair reads 36 KB and writes 4 for its 32 products of a head of 128, which
-// is as much as a compute unit's LDS gives in the products' own time.  Two pairs to a
-// workgroup leave two workgroups on a compute unit that do not wait for each other:
-// sixteen ragged rollouts 649 us (four pairs and a deeper ring 645, six at three waves a SIMD 690), 200
-// sequences of at most 30 positions, backward as a whole, 68 us where four pairs take 90.
+// is as much as a compute unit's LDS gives in the products' own time.  Sixteen ragged
+// rollouts, 32 heads of 128 on 8: 626 us; one sequence of 8703, 16 heads of 64 on 4: 360.  Two
+// pairs to a workgroup leave two or three workgroups on a compute unit that do not wait for
+// each other; four pairs took 645 (and 90 us for the backward pass of 200 sequences of at
+// most 30, now 68), six pairs at three waves a SIMD 690.  One tile less in LDS, the
+// probabilities handed over in the middle of a step at a second meeting, took 676 and 383.
 //
 // Where the tiles of keys are few, a workgroup takes one part of the group's heads and
 // writes float32 sums, which flash_join_kernel adds up.
@@ -681,8 +684,8 @@ __global__ __launch_bounds__(128 * kPairs, (HD == 64 ? 3 : 2)) void flash_dkv_pa
   using S = Stager<bf16_t, HD, 32, kPairs>;
   constexpr int TILE = 32 * O::ROW, TURNS = 3;
   __shared__ __align__(16) char lds[TURNS][2][TILE];       // [turn][queries, output gradients]
-  __shared__ __align__(16) float prob[2][kPairs][1024];     // [turn][pair]: probabilities in lane order
-  __shared__ __align__(16) float stat[TURNS][2 * kPairs][64];         // [turn][wave]: log-sum-exps, negated deltas
+  __shared__ __align__(16) float prob[2][kPairs][1024];    // [step's parity][pair]: probabilities in lane order
+  __shared__ __align__(16) float stat[TURNS][2 * kPairs][64];  // [turn][wave]: log-sum-exps, negated deltas
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool second = wave >= kPairs;
   const int h = lane >> 5, col = lane & 31, pair = second ? wave - kPairs : wave;
@@ -718,7 +721,7 @@ __global__ __launch_bounds__(128 * kPairs, (HD == 64 ? 3 : 2)) void flash_dkv_pa
       src_stat = head_stat += a.N;
     }
   };
-  if (total > 0) load(0);
+  load(0);
   const typename O::Lanes at = O::lanes(lane);
   const float s2 = a.scale * kLog2e;
   f32x16_t acc[HD / 32];
