@@ -838,6 +838,13 @@ int flash_parts(int N, int n_seqs, int nq, int nkv, int hd, int dtype) {
   return dtype == DT_BF16 && hd >= 64 && cut ? nq / nkv : 1;
 }
 
+int64_t flash_blocks(int N, int n_seqs, int nq, int nkv) {
+  // per = 128 / together positions to a slot and nq / together workgroups; of pairs, 64 positions
+  // and nkv * parts <= nq
+  const int64_t forward = ((int64_t)N / 128 + n_seqs + 1) * nq, pairs = ((int64_t)N / 64 + n_seqs) * nq;
+  return forward > pairs ? forward : pairs;
+}
+
 #define TANDEM_FLASH_DISPATCH(fn)                                                            \
   switch (hd) {                                                                              \
     case 32: return dtype == DT_BF16 ? fn<bf16_t, 32>(a, st) : fn<float, 32>(a, st);         \

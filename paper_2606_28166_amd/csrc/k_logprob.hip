@@ -483,6 +483,12 @@ int logprob_splits(int R, int V, int* chunk) {
   return (V + c - 1) / c;
 }
 
+int64_t logprob_blocks(int R, int V) {
+  const int64_t forward = V <= 2048 ? ((int64_t)R + 3) / 4 : R;
+  const int64_t backward = (int64_t)R * ((V + kGradChunk - 1) / kGradChunk);
+  return forward > backward ? forward : backward;
+}
+
 hipError_t launch_logprob(const LogprobArgs& a, int dtype, hipStream_t st) {
   if (dtype == DT_BF16) return a.zr ? run<bf16_t, true>(a, st) : run<bf16_t, false>(a, st);
   return a.zr ? run<float, true>(a, st) : run<float, false>(a, st);

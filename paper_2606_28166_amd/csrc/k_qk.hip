@@ -243,8 +243,8 @@ int head_phases(int N, int nq, int nkv, int hd) {
 
 template <typename T, int HD>
 hipError_t run(const QkArgs& a, hipStream_t st) {
-  const int ph = head_phases(a.N, a.nq, a.nkv, HD), rows = 256 / (HD / 16) / ph;
-  qk_kernel<T, HD><<<(a.N + rows - 1) / rows, 256, 0, st>>>(a, ph);
+  const int ph = head_phases(a.N, a.nq, a.nkv, HD);
+  qk_kernel<T, HD><<<(unsigned)qk_blocks(a.N, a.nq, a.nkv, HD), 256, 0, st>>>(a, ph);
   return hipGetLastError();
 }
 template <typename T, int HD>
@@ -259,10 +259,13 @@ hipError_t run_backward(const QkArgs& a, hipStream_t st) {
 
 }  // namespace
 
-int qk_backward_blocks(int N, int nq, int nkv, int hd) {
+int64_t qk_blocks(int N, int nq, int nkv, int hd) {
   const int rows = 256 / (hd / 16) / head_phases(N, nq, nkv, hd);
-  const int most = N > 0 ? (N + rows - 1) / rows : 1;      // no rows: one workgroup writes sums of 0
-  return most < 1024 ? most : 1024;
+  return ((int64_t)N + rows - 1) / rows;
+}
+int qk_backward_blocks(int N, int nq, int nkv, int hd) {
+  const int64_t most = N > 0 ? qk_blocks(N, nq, nkv, hd) : 1;        // no rows: one workgroup writes sums of 0
+  return most < 1024 ? (int)most : 1024;
 }
 
 #define TANDEM_QK_DISPATCH(fn)                                             \

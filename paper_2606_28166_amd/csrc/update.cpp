@@ -14,7 +14,8 @@ using namespace tandem;
 
 namespace {
 
-constexpr int64_t kMaxGrid = 0x7FFFFFFF;      // workgroups of a launch
+constexpr int64_t kMaxGrid = 0xFFFFFFFFll / 256;   // workgroups of a launch: fewer than 2^32 threads, up to 256 each
+constexpr int32_t kMaxRows = 1 << 30;              // indexes of rows past the last of a workgroup stay in 31 bits
 
 __attribute__((format(printf, 2, 3))) tandem_status refuse(tandem_status s, const char* fmt, ...) {
   char b[256];
@@ -82,6 +83,8 @@ tandem_status logprob_check(const char* who, const tandem_logprob_cfg* c, Logpro
   if (!c) return refuse(TANDEM_E_ARG, "%s: cfg is NULL", who);
   if (c->rows < 0 || c->vocab < 1) return refuse(TANDEM_E_SHAPE, "%s: rows must be >= 0 and vocab >= 1", who);
   if (c->vocab > (1 << 30)) return refuse(TANDEM_E_SHAPE, "%s: vocab must be at most 2^30", who);
+  if (logprob_blocks(c->rows, c->vocab) > kMaxGrid)
+    return refuse(TANDEM_E_SHAPE, "%s: rows * vocab exceeds what one launch covers", who);
   if (!dtype_ok(c->dtype)) return refuse(TANDEM_E_ARG, "%s: dtype must be TANDEM_BF16 or TANDEM_F32", who);
   if (!(c->temperature > 0.f) || !std::isfinite(c->temperature) || !std::isfinite(1.f / c->temperature))
     return refuse(TANDEM_E_ARG, "%s: temperature must be positive, with a finite reciprocal", who);
@@ -103,6 +106,7 @@ tandem_status logprob_check(const char* who, const tandem_logprob_cfg* c, Logpro
 
 tandem_status heads_check(const char* who, int32_t rows, int32_t nq, int32_t nkv, int32_t hd, int32_t dtype) {
   if (rows < 0 || nq < 1 || nkv < 1) return refuse(TANDEM_E_SHAPE, "%s: rows must be >= 0 and heads >= 1", who);
+  if (rows > kMaxRows) return refuse(TANDEM_E_SHAPE, "%s: rows must be at most 2^30", who);
   if (nq % nkv != 0) return refuse(TANDEM_E_SHAPE, "%s: n_q_heads must be a multiple of n_kv_heads", who);
   if (hd != 32 && hd != 64 && hd != 128)
     return refuse(TANDEM_E_UNSUPPORTED, "%s: head_dim %d unsupported (32, 64 or 128)", who, hd);
@@ -131,6 +135,8 @@ tandem_status qk_check(const char* who, const tandem_qk_cfg* c, QkArgs* a) {
     return s;
   if ((s = stride_check(who, "q_stride", c->q_stride, c->n_q_heads * hd, c->dtype)) != TANDEM_OK) return s;
   if ((s = stride_check(who, "k_stride", c->k_stride, c->n_kv_heads * hd, c->dtype)) != TANDEM_OK) return s;
+  if (qk_blocks(c->rows, c->n_q_heads, c->n_kv_heads, c->head_dim) > kMaxGrid)
+    return refuse(TANDEM_E_SHAPE, "%s: rows exceed what one launch covers", who);
   *a = QkArgs{};
   a->N = c->rows; a->nq = c->n_q_heads; a->nkv = c->n_kv_heads; a->hd = c->head_dim;
   a->ld = c->qkv_stride; a->ldq = c->q_stride; a->ldk = c->k_stride;
@@ -156,10 +162,8 @@ tandem_status attention_check(const char* who, const tandem_attention_cfg* c, bo
       {"dk_stride", c->dk_stride, kv},    {"dv_stride", c->dv_stride, kv}};
   for (int i = 0; i < (backward ? 8 : 4); ++i)
     if ((s = stride_check(who, st[i].what, st[i].stride, st[i].least, c->dtype)) != TANDEM_OK) return s;
-  // a slot per 32 positions and sequence at most, per query head at most
-  if (((int64_t)c->rows / 32 + c->n_seqs + 1) * c->n_q_heads > kMaxGrid ||
-      ((int64_t)c->rows * c->n_q_heads) / 16 > kMaxGrid)
-    return refuse(TANDEM_E_SHAPE, "%s: rows * n_q_heads exceeds what one launch covers", who);
+  if (flash_blocks(c->rows, c->n_seqs, c->n_q_heads, c->n_kv_heads) > kMaxGrid)
+    return refuse(TANDEM_E_SHAPE, "%s: rows and sequences times heads exceed what one launch covers", who);
   *a = FlashArgs{};
   a->N = c->rows; a->n_seqs = c->n_seqs; a->nq = c->n_q_heads; a->nkv = c->n_kv_heads;
   a->scale = c->scale;
@@ -259,8 +263,6 @@ tandem_status tandem_token_logprob_backward(const tandem_logprob_cfg* cfg, const
   if (s != TANDEM_OK) return s;
   if (cfg->grad_stride < cfg->vocab) return refuse(TANDEM_E_SHAPE, "%s: grad_stride is below vocab", who);
   if (g_kl && cfg->ref_stride < cfg->vocab) return refuse(TANDEM_E_SHAPE, "%s: ref_stride is below vocab", who);
-  if ((int64_t)a.R * ((a.V + 8191) / 8192) > kMaxGrid)
-    return refuse(TANDEM_E_SHAPE, "%s: rows * vocab exceeds what one launch covers", who);
   if (a.R == 0) return TANDEM_OK;
   if (!logits || !tokens || !lse || !g_logp || !grad || (g_kl && (!logits_ref || !kl || !lse_diff)))
     return refuse(TANDEM_E_ARG, "%s: a required pointer is NULL", who);

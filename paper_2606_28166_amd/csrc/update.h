@@ -17,8 +17,7 @@ struct LogprobArgs {
   const int32_t* tok;
   float inv_t;                             // 1 / temperature
   int eos; float bias, bias_r;             // eos < 0: no bias
-  float* logp; float* lse; float* kl; float* diff;                     // forward outputs
-  const float* in_lse; const float* in_kl; const float* in_diff;       // backward inputs
+  float* logp; float* lse; float* kl; float* diff;                     // outputs, of the backward pass inputs
   const float* g_logp; const float* g_kl;
   void* grad;
   float* part;                             // [R][splits][kLogprobPart]: partials of a row cut into splits
@@ -27,6 +26,7 @@ struct LogprobArgs {
 constexpr int kLogprobPart = 5;            // max, sum; weighted difference; the reference's max, sum
 // How the forward pass cuts a row: the number of parts (1: no workspace).
 int logprob_splits(int R, int V, int* chunk);
+int64_t logprob_blocks(int R, int V);      // workgroups of the largest launch
 hipError_t launch_logprob(const LogprobArgs& a, int dtype, hipStream_t st);
 hipError_t launch_logprob_backward(const LogprobArgs& a, int dtype, hipStream_t st);
 
@@ -44,6 +44,7 @@ struct QkArgs {
   float* dgq; float* dgk;
   float* part;                             // [blocks][2][hd]: the gains' gradients by workgroup
 };
+int64_t qk_blocks(int N, int nq, int nkv, int hd);         // workgroups of the forward pass
 int qk_backward_blocks(int N, int nq, int nkv, int hd);   // workgroups of the backward pass
 hipError_t launch_qk(const QkArgs& a, int dtype, hipStream_t st);
 hipError_t launch_qk_backward(const QkArgs& a, int dtype, hipStream_t st);
@@ -61,6 +62,7 @@ struct FlashArgs {
   float* sums;                             // and [dV, dK][parts][N][nkv][hd], where a group's heads are cut into parts
 };
 int flash_parts(int N, int n_seqs, int nq, int nkv, int hd, int dtype);
+int64_t flash_blocks(int N, int n_seqs, int nq, int nkv);  // workgroups of a launch, at most
 hipError_t launch_flash(const FlashArgs& a, int hd, int dtype, hipStream_t st);
 hipError_t launch_flash_backward(const FlashArgs& a, int hd, int dtype, hipStream_t st);
 

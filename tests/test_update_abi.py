@@ -194,3 +194,21 @@ def test_engine_refuses_cpu_tensors_and_shapes():
         E.AdamW([])
     with pytest.raises(ValueError):
         E.AdamW([torch.zeros(4)])
+
+
+def test_refuses_more_than_a_launch_covers():
+    """A launch has fewer than 2^32 threads; indexes of rows stay in 31 bits."""
+    big = 2**31 - 1
+    for c in (_logprob(rows=big, vocab=1, logits_stride=1, ref_stride=1, grad_stride=1),
+              _logprob(rows=1 << 24, vocab=5000, logits_stride=5000, ref_stride=5000, grad_stride=5000),
+              _logprob(rows=1 << 20, vocab=200000, logits_stride=200000, ref_stride=200000, grad_stride=200000)):
+        assert _logprob_call(c) == L.E_SHAPE
+        assert _status(L.lib.tandem_token_logprob_backward, C.byref(c), P, P, P, P, P, P, P, P, P, None) == L.E_SHAPE
+    for c in (_qk(rows=big), _qk(rows=(1 << 30) + 1), _qk(rows=1 << 30)):
+        assert _status(L.lib.tandem_qk_norm_rope, C.byref(c), P, P, P, P, P, P, None) == L.E_SHAPE
+        assert _status(L.lib.tandem_qk_norm_rope_backward, C.byref(c), P, P, P, P, P, P, P, P, P, WS, 1 << 20,
+                       None) == L.E_SHAPE
+    for c in (_attn(rows=big), _attn(rows=1 << 30), _attn(n_seqs=big), _attn(n_seqs=1 << 23)):
+        assert _status(L.lib.tandem_attention, C.byref(c), P, P, P, P, P, P, None) == L.E_SHAPE
+        assert _status(L.lib.tandem_attention_backward, C.byref(c), P, P, P, P, P, P, P, P, P, P, WS, 1 << 20,
+                       None) == L.E_SHAPE
