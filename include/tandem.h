@@ -308,7 +308,9 @@ tandem_status tandem_grpo_loss_noalloc(const tandem_grpo_cfg* cfg, const float* 
  * current for the call), allocates nothing and may be captured into a HIP
  * graph.  Workspaces are sized by the matching *_workspace_size call, 256-byte
  * aligned, need no initialisation, and must not be shared by calls that may
- * overlap (captured graphs that may run together included).  Results do not
+ * overlap (captured graphs that may run together included).  Outputs and the
+ * workspace overlap neither inputs nor each other, except where a call says that
+ * they may.  Results do not
  * depend on the order in which the device runs its work.  Errors are reported
  * through tandem_last_error(NULL); a call that fails before its first launch
  * has written nothing.
@@ -411,8 +413,9 @@ tandem_status tandem_qk_norm_rope_backward(const tandem_qk_cfg* cfg, const void*
  * offsets[0] and from offsets[n_seqs] on belong to no sequence and their
  * outputs are left as they are.  bf16 inputs: products on the matrix cores
  * with float32 sums, probabilities rounded to bf16 for the value product.
- * Values must be finite: a NaN or infinity in one row of v reaches other rows
- * of the same sequence.
+ * The inputs must be finite: a NaN or infinity in a row of v, in the backward
+ * pass of any input, may reach other rows of the same sequence, never another
+ * sequence.
  * Heads of a row are contiguous ([n][head_dim]); arrays are 16-byte aligned
  * and strides multiples of 16 bytes, so q, k and v may be columns of one
  * projection. */
@@ -451,7 +454,8 @@ tandem_status tandem_attention_backward(const tandem_attention_cfg* cfg, const v
  * arenas of arena_elems floats in which tensor i occupies
  * [state_offset, state_offset + n), state_offset a multiple of 4; master NULL:
  * no master copies.  tensors is a HOST array that is read during the call.
- * Weights, gradients and arenas do not overlap. */
+ * Weights, gradients, arenas and the tensors' places in the arenas do not
+ * overlap. */
 typedef struct {
   void* param;                     /* weights, updated in place */
   const void* grad;

@@ -219,6 +219,14 @@ _DT = {torch.bfloat16: L.BF16, torch.float32: L.F32}
 _lib = L.lib
 
 
+_MOST = 0x7FFFFFFF      # the library counts rows in 32 bits
+
+
+def _count(who: str, n: int) -> None:
+    if n > _MOST:
+        raise ValueError(f"{who}: {n} rows are too many")
+
+
 def _same(who: str, name: str, t: torch.Tensor, dtype, shape, dev) -> None:
     """A contiguous tensor of this dtype, shape and device."""
     if t.dtype is not dtype or t.shape != shape or t.device != dev or not t.is_contiguous():
@@ -272,10 +280,10 @@ def _ptr(t: Optional[torch.Tensor]):
 
 
 def _workspace(t: Optional[torch.Tensor], need: int, dev) -> Optional[torch.Tensor]:
-    """t if it is large enough, a new one otherwise; None when nothing is needed."""
+    """t if it is large enough and contiguous, a new one otherwise; None when nothing is needed."""
     if need == 0:
         return None
-    if t is None or t.numel() * t.element_size() < need or t.device != dev:
+    if t is None or t.numel() * t.element_size() < need or t.device != dev or not t.is_contiguous():
         return torch.empty(need, dtype=torch.uint8, device=dev)
     return t
 
@@ -286,6 +294,7 @@ def _logprob_cfg(who, logits, tokens, ref, temperature, eos_id, eos_bias, eos_bi
         raise ValueError(f"{who}: logits must be a bfloat16 or float32 tensor [rows][vocab]")
     shape, dev = logits.shape, logits.device
     R, V = shape
+    _count(who, max(R, V))
     _gpu(dev)
     ld = _rows(who, "logits", logits, dt, shape, dev)
     ldr = _rows(who, "ref", ref, dt, shape, dev) if ref is not None else V
@@ -355,6 +364,7 @@ def _qk_cfg(who, qkv, positions, n_q, n_kv, theta, eps, q_gain, k_gain):
     if qkv.dim() != 2 or dt not in _DT or n_q < 1 or n_kv < 1 or qkv.shape[1] % (n_q + 2 * n_kv) != 0:
         raise ValueError(f"{who}: qkv must be a bfloat16 or float32 tensor [rows][(n_q + 2 n_kv) * head_dim]")
     N, cols = qkv.shape
+    _count(who, N)
     hd = cols // (n_q + 2 * n_kv)
     _gpu(dev)
     ld = _rows(who, "qkv", qkv, dt, qkv.shape, dev)
@@ -426,6 +436,7 @@ def _attention_cfg(who, q, k, v, offsets, scale):
     _gpu(dev)
     N, nq, hd = q.shape
     nkv = k.shape[1]
+    _count(who, max(N, offsets.numel()))
     heads = (N, nkv, hd)
     if offsets.dim() != 1 or offsets.numel() < 1:
         raise ValueError(f"{who}: offsets must hold at least one entry")
@@ -494,7 +505,8 @@ class AdamW:
     is what the update is applied to (a bfloat16 weight is its rounding; at
     learning rates of 1e-6 it would otherwise not move).
 
-    params: contiguous bfloat16 or float32 tensors on one GPU, updated in place.
+    params: contiguous bfloat16 or float32 tensors on one GPU that share no
+    memory, updated in place.
     weight_decay: one number, or one per tensor.  max_norm > 0 clips by the
     global norm of the gradients.  master None: where any weight is bfloat16.
     state: what state() returned, to resume (its tensors are used, not copied)."""
@@ -508,7 +520,9 @@ class AdamW:
             raise ValueError("AdamW: no tensors")
         self.dev = self.params[0].device
         _gpu(self.dev)
-        self._check_params()
+        self._shapes = [p.shape for p in self.params]
+        self._types = [p.dtype for p in self.params]
+        self._places = self._check_params()
         n = len(self.params)
         decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * n
         if len(decay) != n:
@@ -522,6 +536,8 @@ class AdamW:
         if state is not None:
             self.steps, self.m, self.v, self.master = int(state["step"]), state["m"], state["v"], state["master"]
             for name in ("m", "v", "master"):
+                if state[name] is None and name != "master":
+                    raise ValueError(f"AdamW: the state has no {name}")
                 if state[name] is not None:
                     _same("AdamW", name, state[name], torch.float32, (total,), self.dev)
         else:
@@ -533,9 +549,7 @@ class AdamW:
             self.master = torch.zeros(total, dtype=torch.float32, device=self.dev) if master else None
             if master:
                 for p, o in zip(self.params, self.offsets):
-                    self.master[o:o + p.numel()].copy_(p.reshape(-1))
-        self._shapes = [p.shape for p in self.params]
-        self._types = [p.dtype for p in self.params]
+                    self.master[o:o + p.numel()].copy_(p.detach().reshape(-1))
         # the tensors' table as the library reads it, and a view of it by columns
         self._table = (L.AdamwTensor * n)(*[
             L.AdamwTensor(p.data_ptr(), None, p.numel(), o, float(w), _DT[p.dtype], _DT[p.dtype])
@@ -545,10 +559,20 @@ class AdamW:
              for name, t in L.AdamwTensor._fields_]))
         self._grad_types = self._types
 
-    def _check_params(self) -> None:
-        for p in self.params:
+    def _check_params(self) -> list:
+        """The weights' addresses; refuses weights that a step cannot write."""
+        spans = []
+        for p, t, s in zip(self.params, self._types, self._shapes):
             if p.dtype not in _DT or p.device != self.dev or not p.is_contiguous():
                 raise ValueError(f"AdamW: weights must be contiguous bfloat16 or float32 tensors on {self.dev}")
+            if p.dtype != t or p.shape != s:
+                raise ValueError("AdamW: a weight's type or shape has changed")
+            if p.numel() > 0:
+                spans.append((p.data_ptr(), p.data_ptr() + p.numel() * p.element_size()))
+        spans.sort()
+        if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
+            raise ValueError("AdamW: weights share memory")
+        return [p.data_ptr() for p in self.params]
 
     def state(self) -> dict:
         """The optimizer's state, to be saved and given to another AdamW."""
@@ -571,9 +595,10 @@ class AdamW:
             self._columns["grad_dtype"] = [_DT[t] for t in types]
             self._grad_types = types
         # a weight whose storage was replaced since the last step is followed
-        if [p.dtype for p in self.params] != self._types or [p.shape for p in self.params] != self._shapes:
-            raise ValueError("AdamW: a weight's type or shape has changed")
-        self._columns["param"] = [p.data_ptr() for p in self.params]
+        if ([p.data_ptr() for p in self.params] != self._places or not all([p.is_contiguous() for p in self.params])
+                or [p.dtype for p in self.params] != self._types or [p.shape for p in self.params] != self._shapes):
+            self._places = self._check_params()
+            self._columns["param"] = self._places
         self._columns["grad"] = [g.data_ptr() for g in grads]
         b1, b2 = self.betas
         cfg = L.AdamwCfg(lr, b1, b2, self.eps, self.max_norm, self.steps + 1, self.elems)

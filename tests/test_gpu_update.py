@@ -419,6 +419,32 @@ def test_attention(lens, nq, nkv, hd, dt):
         assert torch.equal(again[name][rows], b[name][rows]), name
 
 
+@pytest.mark.parametrize("nq,nkv,hd", [(8, 4, 128), (16, 4, 64), (4, 2, 32)])
+@pytest.mark.parametrize("dt", [BF, F32], ids=["bf16", "f32"])
+def test_attention_of_many_short_sequences(nq, nkv, hd, dt):
+    """A group's heads in one workgroup (enough tiles of keys), sequences found by length
+    (64 of them) and by their offsets (65); rows of no sequence hold NaN and reach nothing."""
+    from paper_2606_28166_amd import engine as E
+    for n in (64, 65):
+        _say("attention, many", n, nq, nkv, hd, dt)
+        offs = list(itertools.accumulate([2] + [(53 * i) % 131 for i in range(n)]))
+        N = offs[-1] + 7
+        q, k, v, dout = _attention_inputs(N, nq, nkv, hd, dt, n)
+        for x in (q, k, v, dout):
+            x[:2] = math.nan
+            x[offs[-1]:] = math.nan
+        scale = float(torch.tensor(hd ** -0.5, dtype=F32))
+        ref, tol = _attention_reference(q, k, v, dout, offs, scale)
+        o = torch.tensor(offs, dtype=torch.int32, device=DEV)
+        rows = slice(offs[0], offs[-1])
+        f = E.attention(q, k, v, o, out=torch.full_like(q, math.nan))
+        _within(f["out"][rows], ref["out"][rows], tol["out"][rows], "out")
+        _within(f["lse"][:, rows], ref["lse"][:, rows], tol["lse"][:, rows], "lse")
+        b = E.attention_backward(dout, q, k, v, f["out"], f["lse"], o)
+        for name in ("dq", "dk", "dv"):
+            _within(b[name][rows], ref[name][rows], tol[name][rows], name)
+
+
 def test_attention_gradient_by_differences():
     """float32: the gradient of sum(w out) against central differences of the
     definition in 64 bits."""
@@ -589,6 +615,73 @@ def test_adamw_resumes_and_repeats():
 
     a, b = run(2), run(9)
     assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_adamw_of_trainable_weights():
+    """Weights that require gradients: the state stays free of any autograd graph, and the
+    step equals that of plain tensors."""
+    from paper_2606_28166_amd import engine as E
+
+    def run(make):
+        g = _gen(3)
+        p = [make(torch.randn(s, generator=g, device=DEV).to(BF)) for s in ((40, 30), (7,))]
+        opt = E.AdamW(p, max_norm=1.0, weight_decay=0.1)
+        for x in p:
+            x.grad = torch.randn(x.shape, generator=g, device=DEV).to(BF)
+        opt.step([x.grad for x in p], 1e-2)
+        return p, opt
+
+    plain, a = run(lambda x: x)
+    train, b = run(lambda x: torch.nn.Parameter(x))
+    assert b.master.grad_fn is None and not b.master.requires_grad and all(x.requires_grad for x in train)
+    for x, y in zip(plain + [a.m, a.v, a.master], train + [b.m, b.v, b.master]):
+        assert torch.equal(x, y.detach())
+
+
+def test_adamw_refuses_weights_it_cannot_update():
+    """Weights that share memory would be written by two workgroups at once; a weight moved
+    since the last step is followed, unless it no longer is what the step can write."""
+    from paper_2606_28166_amd import engine as E
+    w = torch.zeros(64, device=DEV)
+    for params in ([w, w], [w, w[32:]], [w[:40], w[39:]], [w[1:2], w, w[:0]]):
+        with pytest.raises(ValueError):
+            E.AdamW(params)
+    E.AdamW([w[:32], w[32:], w[:0], w[:0]])
+    a, b = torch.zeros((8, 8), device=DEV), torch.zeros(5, device=DEV)
+    opt = E.AdamW([a, b])
+    grads = [torch.ones_like(a), torch.ones_like(b)]
+    opt.step(grads, 1e-3)
+    a.data = a.data.clone()
+    opt.step(grads, 1e-3)
+    assert (a == a[0, 0]).all() and float(a[0, 0]) < -1.5e-3
+    kept, steps = a.data, opt.steps
+    for moved in (kept.t(), kept[:1, :1].expand(8, 8), kept.cpu(), kept.double(), kept.flatten()):
+        a.data = moved
+        with pytest.raises(ValueError):
+            opt.step(grads, 1e-3)
+    a.data = kept
+    b.data = kept.view(-1)[3:8]                                 # now within the other weight
+    with pytest.raises(ValueError):
+        opt.step(grads, 1e-3)
+    assert opt.steps == steps
+    for state in (dict(opt.state(), m=None), dict(opt.state(), v=opt.v[:64])):
+        with pytest.raises(ValueError):
+            E.AdamW([a, torch.zeros(5, device=DEV)], state=state)
+
+
+def test_workspaces_given():
+    """A given workspace is used where it is large enough and contiguous, replaced otherwise."""
+    from paper_2606_28166_amd import engine as E
+    z, zr, tok, _, _ = _logprob_inputs(2, 40000, F32, 1)
+    want = E.token_logprob(z, tok, ref=zr)
+    for ws in (torch.full((1 << 16,), 255, dtype=torch.uint8, device=DEV),
+               torch.full((1,), 255, dtype=torch.uint8, device=DEV).expand(1 << 16),
+               torch.full((1 << 17,), 255, dtype=torch.uint8, device=DEV)[::2],
+               torch.full((3,), 255, dtype=torch.uint8, device=DEV)):
+        keep = ws.clone()
+        got = E.token_logprob(z, tok, ref=zr, workspace=ws)
+        assert all(torch.equal(got[n], want[n]) for n in want)
+        assert torch.equal(ws, keep) != (ws.is_contiguous() and ws.numel() > 1000)
 
 
 # ------------------------------------------------------------------ streams, graphs, several at once
