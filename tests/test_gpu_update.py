@@ -212,6 +212,34 @@ def test_logprob_masked_entries(dt, V):
     assert (E.token_logprob_backward(z, tok, r, gl) == 0).all()
 
 
+def test_logprob_gradient_by_differences():
+    """float32: the gradient of sum(g logp + k kl) against central differences of the
+    definition in 64 bits, with temperature and the rollout's EOS bias."""
+    from paper_2606_28166_amd import engine as E
+    R, V, T, eos, b, br = 4, 37, 0.7, 5, 1.5, -0.5
+    z, zr, tok, gl, gk = _logprob_inputs(R, V, F32, 2)
+    kw = dict(temperature=T, eos_id=eos, eos_bias=b, eos_bias_ref=br)
+    f = E.token_logprob(z, tok, ref=zr, **kw)
+    got = E.token_logprob_backward(z, tok, f, gl, g_kl=gk, ref=zr, **kw).cpu().double()
+    x, q = z.cpu().double(), _scores64(zr.cpu(), T, eos, br).log_softmax(1)
+    y, wl, wk = tok.cpu().long()[:, None], gl.cpu().double(), gk.cpu().double()
+
+    def loss(x):
+        lp = _scores64(x, T, eos, b).log_softmax(1)
+        return float((wl * lp.gather(1, y)[:, 0] + wk * (lp.exp() * (lp - q)).sum(1)).sum())
+
+    step = 1e-5
+    flat = x.view(-1)
+    for at in range(flat.numel()):
+        keep = float(flat[at])
+        flat[at] = keep + step
+        up = loss(x)
+        flat[at] = keep - step
+        down = loss(x)
+        flat[at] = keep
+        assert abs((up - down) / (2 * step) - float(got.view(-1)[at])) <= 1e-4, at
+
+
 def test_logprob_far_rows():
     """Rows whose offset passes 2^31 elements."""
     from paper_2606_28166_amd import engine as E
@@ -301,6 +329,42 @@ def test_qk_norm_rope(nq, nkv, hd, N, far, dt, norm):
     fresh = E.qk_norm_rope_backward(qkv, pos, dq, dk, theta, eps, q_gain=gq, k_gain=gk)
     assert torch.equal(fresh["dqkv"][:, :(nq + nkv) * hd], mark[:, :(nq + nkv) * hd])
     assert (fresh["dqkv"][:, (nq + nkv) * hd:] == 0).all()
+
+
+def test_qk_gradient_by_differences():
+    """float32: the gradients of sum(wq q) + sum(wk k) against central differences of the
+    definition in 64 bits."""
+    from paper_2606_28166_amd import engine as E
+    nq, nkv, hd, N, theta, eps = 2, 1, 32, 3, 1e4, 1e-6
+    g = _gen(6)
+    qkv = torch.randn((N, (nq + 2 * nkv) * hd), generator=g, device=DEV)
+    pos = torch.tensor([0, 5, 1000], dtype=torch.int32, device=DEV)
+    gq, gk = (1 + 0.3 * torch.randn((hd,), generator=g, device=DEV) for _ in range(2))
+    wq, wk = torch.randn((N, nq, hd), generator=g, device=DEV), torch.randn((N, nkv, hd), generator=g, device=DEV)
+    b = E.qk_norm_rope_backward(qkv, pos, wq, wk, theta, eps, q_gain=gq, k_gain=gk)
+    x = [t.cpu().double().contiguous() for t in (qkv, gq, gk)]
+    w = torch.cat([wq, wk], 1).cpu().double()
+    a = pos.cpu().double()[:, None] * float(theta) ** (-2.0 * torch.arange(hd // 2, dtype=F64) / hd)
+    cos, sin = a.cos()[:, None], a.sin()[:, None]
+
+    def loss(qkv, gq, gk):
+        h = qkv[:, :(nq + nkv) * hd].reshape(N, nq + nkv, hd)
+        n = h / (h.pow(2).mean(2, keepdim=True) + eps).sqrt() * torch.cat([gq.expand(nq, hd), gk.expand(nkv, hd)])
+        u, v = n[..., :hd // 2], n[..., hd // 2:]
+        return float((torch.cat([u * cos - v * sin, v * cos + u * sin], 2) * w).sum())
+
+    step = 1e-5
+    for which, name in enumerate(("dqkv", "dq_gain", "dk_gain")):
+        flat = x[which].view(-1)
+        for at in range(0, flat.numel(), 7):
+            keep = float(flat[at])
+            flat[at] = keep + step
+            up = loss(*x)
+            flat[at] = keep - step
+            down = loss(*x)
+            flat[at] = keep
+            # the value columns' gradient is 0, as the loss does not read them
+            assert abs((up - down) / (2 * step) - float(b[name].reshape(-1)[at])) <= 1e-4, (name, at)
 
 
 def test_qk_no_rows_clears_the_gains():
@@ -735,6 +799,32 @@ def test_update_graph_replays():
         assert all(torch.equal(x, y) for x, y in zip(run(), want))
 
 
+def test_attention_graph_of_other_offsets():
+    """The offsets are read on the device: one captured call serves other lengths in the
+    same rows."""
+    from paper_2606_28166_amd import engine as E
+    N, nq, nkv, hd = 500, 8, 2, 64
+    q, k, v, dout = _attention_inputs(N, nq, nkv, hd, BF, 21)
+    offs = torch.tensor([0, 100, 101, 500], dtype=torch.int32, device=DEV)
+
+    def run():
+        f = E.attention(q, k, v, offs)
+        return f, E.attention_backward(dout, q, k, v, f["out"], f["lse"], offs)
+
+    run()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        f, b = run()
+    for to in ([0, 500, 500, 500], [0, 0, 1, 500], [0, 250, 499, 500], [0, 100, 101, 500]):
+        offs.copy_(torch.tensor(to, dtype=torch.int32))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        ff, bb = run()
+        for x, y in ((f, ff), (b, bb)):
+            assert all(torch.equal(x[n], y[n]) for n in x), to
+
+
 def test_update_on_two_streams():
     """Two streams at once, neither the default one."""
     runs = [_all_ops(s)[0] for s in (11, 12)]
@@ -755,7 +845,6 @@ def test_adamw_graph_replays():
     """A captured step repeats that step, its number included."""
     from paper_2606_28166_amd import engine as E
     _, opt, params, grads = _all_ops(6)
-    side = torch.cuda.Stream()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         norm = opt.step(grads, 1e-3)
