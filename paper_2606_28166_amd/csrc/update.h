@@ -23,7 +23,7 @@ struct LogprobArgs {
   float* part;                             // [R][splits][kLogprobPart]: partials of a row cut into splits
   int splits, chunk;                       // forward: a row's parts, and their length in entries
 };
-constexpr int kLogprobPart = 5;            // max, sum; weighted difference; the reference's max, sum
+constexpr int kLogprobPart = 8;            // floats: a part's two maxima and three sums of 64 bits
 // How the forward pass cuts a row: the number of parts (1: no workspace).
 int logprob_splits(int R, int V, int* chunk);
 int64_t logprob_blocks(int R, int V);      // workgroups of the largest launch
