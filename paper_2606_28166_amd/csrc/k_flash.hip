@@ -370,9 +370,10 @@ struct Softmax {
   }
 };
 
-// Bound by latency more than by any one pipe: what counts is the waves a SIMD holds, so the
-// tiles are of 32 keys and the code keeps nothing ahead.  Heads of 128 take 161 registers,
-// three waves a SIMD: sixteen ragged rollouts (32 heads on 8) 279 us, 0.9 PFLOP/s.  Two waves with
+// Bound by latency more than by any one pipe (the matrix pipe is busy 56% of the cycles): what
+// counts is the waves a SIMD holds, so the tiles are of 32 keys and the code keeps nothing
+// ahead.  Heads of 128 take 161 registers, three waves a SIMD: sixteen ragged rollouts (32 heads
+// on 8) 278 us, 0.9 PFLOP/s.  Two waves with
 // tiles of 64 and the scores, exponentials and value products of three blocks
 // interleaved in each took 314, two without that 325.
 template <typename T, int HD>
@@ -453,8 +454,18 @@ __device__ __forceinline__ void dq_tile(f32x16_t* dq, const char* __restrict__ t
   }
 }
 
+// The pairs' probabilities are held as 2^15 P, in float16 where they pass from wave to wave:
+// 11 bits down to P = 2^-29, 8 times finer than the bf16 to which dS is rounded next (and
+// rounding P itself to bf16 would round dS twice).  The results are scaled back exactly.
+constexpr float kProbScale = 32768.f, kProbBits = 15.f;
+template <typename T, int HD>
+constexpr bool kByPairs = sizeof(T) == 2 && HD >= 64;     // dK and dV by pairs of waves
+
 // dQ, and for the pass over the keys the deltas dout . out (negated) and the log-sum-exps in
 // powers of two, each (row, head) being one lane pair's.
+// The matrix pipe is busy 50% (heads of 128) and 65% (64) of the cycles: sixteen ragged rollouts
+// 392 to 420 us as the clock allows, one sequence of 8703 235.  Two waves a SIMD; tiles of 32
+// keys, or four waves a SIMD of heads of 64, take the same time.
 template <typename T, int HD>
 __global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_dq_kernel(FlashArgs a) {
   using O = Ops<T, HD>;
@@ -491,7 +502,7 @@ __global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_dq_kerne
   const float lse2 = a.lse[stat] * kLog2e;
   if (h == 0 && qi < w.len) {      // for the pass over the keys
     a.ndelta[stat] = -delta;
-    a.lse2[stat] = lse2;
+    a.lse2[stat] = kByPairs<T, HD> ? lse2 - kProbBits : lse2;
   }
   const float s2 = a.scale * kLog2e;
   f32x16_t dq[HD / 32];
@@ -602,11 +613,13 @@ __global__ __launch_bounds__(64 * kWaves, 1) void flash_dkv_kernel(FlashArgs a) 
   store_rows<T, HD>(room, reinterpret_cast<T*>(a.dv) + row0 * a.lddv + kv * HD, a.lddv, w.len - k0, dv, 1.f, lane);
 }
 
+typedef _Float16 f16x8_v __attribute__((ext_vector_type(8)));
+
 // A step of the pairs below: 32 queries by a pair's 32 keys.  The first wave's half:
 // P = e^(S - lse), dV^T += dO^T P.
 template <int HD>
 __device__ __forceinline__ void dv_step(f32x16_t* dv, const char* __restrict__ tq, const char* __restrict__ tg,
-                                        const float* __restrict__ lse2, float* __restrict__ prob,
+                                        const float* __restrict__ lse2, f16x8_v* __restrict__ prob,
                                         const typename Ops<bf16_t, HD>::Lanes& at,
                                         const typename Ops<bf16_t, HD>::Right& k, bool edge, int col, float s2, int h,
                                         int lane) {
@@ -621,28 +634,35 @@ __device__ __forceinline__ void dv_step(f32x16_t* dv, const char* __restrict__ t
       if (result_row(i, h) < col) p[i] = 0.f;
   }
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    *reinterpret_cast<f32x4_t*>(prob + 256 * j + 4 * lane) =
-        f32x4_t{p[4 * j], p[4 * j + 1], p[4 * j + 2], p[4 * j + 3]};
+  for (int j = 0; j < 2; ++j) {
+    f16x8_v v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (_Float16)p[8 * j + e];
+    prob[64 * j + lane] = v;
+  }
   O::transposed(dv, tg, at, 0, O::pack(p));
 }
-// The second wave's: dP - delta (the sum begins at -delta), dS = P (dP - delta), dK^T += Q^T dS.
+// The second wave's, first dP - delta of a step (the sum begins at -delta), one step later
+// dS = P (dP - delta), dK^T += Q^T dS.
 template <int HD>
-__device__ __forceinline__ void dk_step(f32x16_t* dk, const char* __restrict__ tq, const char* __restrict__ tg,
-                                        const float* __restrict__ ndelta, const float* __restrict__ prob,
-                                        const typename Ops<bf16_t, HD>::Lanes& at,
-                                        const typename Ops<bf16_t, HD>::Right& v, int h, int lane) {
-  using O = Ops<bf16_t, HD>;
+__device__ __forceinline__ f32x16_t dp_step(const char* __restrict__ tg, const float* __restrict__ ndelta,
+                                            const typename Ops<bf16_t, HD>::Lanes& at,
+                                            const typename Ops<bf16_t, HD>::Right& v, int h) {
   f32x16_t dp;
 #pragma unroll
   for (int i = 0; i < 16; ++i) dp[i] = ndelta[result_row(i, h)];
-  dp = O::by_rows(tg, at, 0, v, dp);
+  return Ops<bf16_t, HD>::by_rows(tg, at, 0, v, dp);
+}
+template <int HD>
+__device__ __forceinline__ void dk_step(f32x16_t* dk, const char* __restrict__ tq, const f16x8_v* __restrict__ prob,
+                                        const f32x16_t& dp, const typename Ops<bf16_t, HD>::Lanes& at, int lane) {
+  using O = Ops<bf16_t, HD>;
   float ds[16];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const f32x4_t p = *reinterpret_cast<const f32x4_t*>(prob + 256 * j + 4 * lane);
+  for (int j = 0; j < 2; ++j) {
+    const f16x8_v p = prob[64 * j + lane];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) ds[4 * j + e] = p[e] * dp[4 * j + e];
+    for (int e = 0; e < 8; ++e) ds[8 * j + e] = (float)p[e] * dp[8 * j + e];
   }
   O::transposed(dk, tq, at, 0, O::pack(ds));
 }
@@ -660,32 +680,33 @@ __device__ __forceinline__ void store_column(float* p, const f32x16_t* acc, floa
 
 // dK and dV of bf16 heads of 64 and 128 by pairs of waves: of each pair's 32 keys one wave
 // forms the probabilities and dV, the other dP and dK.  Each then holds one operand and one
-// accumulator (of heads of 128 two waves fit a SIMD, of 64 three, where one wave with both
-// has it alone), and while one takes exponentials the other feeds the matrix pipe.  The
-// probabilities go through LDS in float32, lane to lane (rounded to bf16 they would round
-// dS twice), and the second wave is one step of 32 queries behind the first, so that a step
-// has one meeting.  Three tiles are in LDS: behind, current, arriving.
+// accumulator: three waves of heads of 128 fit a SIMD, four of 64, where one wave with both
+// has it alone.  The probabilities go through LDS, lane to lane, and the second wave uses
+// those of the step behind, so that a step of 32 queries has one meeting: it forms dP of a
+// step and keeps it over the meeting, and needs the step's queries one step longer.
 //
-// Bound by LDS: a pair reads 36 KB and writes 4 for its 32 products of a head of 128, which
-// is as much as a compute unit's LDS gives in the products' own time.  Sixteen ragged
-// rollouts, 32 heads of 128 on 8: 626 us; one sequence of 8703, 16 heads of 64 on 4: 360.  Two
-// pairs to a workgroup leave two or three workgroups on a compute unit that do not wait for
-// each other; four pairs took 645 (and 90 us for the backward pass of 200 sequences of at
-// most 30, now 68), six pairs at three waves a SIMD 690.  One tile less in LDS, the
-// probabilities handed over in the middle of a step at a second meeting, took 676 and 383.
+// The matrix pipe is busy 50% of the cycles; waves wait at the meetings and for LDS.  What bounds
+// a long run is power: the clock goes down to 1.7 GHz, and a form that took a quarter more
+// cycles ran at 1.9.  Sixteen ragged rollouts, 32 heads of 128 on 8: 585 us; one sequence of
+// 8703, 16 heads of 64 on 4: 354.  With float32 probabilities and both tiles a step longer, so two
+// workgroups to a compute unit, 632 and 359; the second wave in the same step, at a second
+// meeting, 676 and 383; four pairs to a workgroup 645 (90 us for the backward pass of 200
+// sequences of at most 30, now 60), six 690.
 //
 // Where the tiles of keys are few, a workgroup takes one part of the group's heads and
 // writes float32 sums, which flash_join_kernel adds up.
 constexpr int kPairs = 2;
 
 template <int HD>
-__global__ __launch_bounds__(128 * kPairs, (HD == 64 ? 3 : 2)) void flash_dkv_pair_kernel(FlashArgs a, int parts) {
+__global__ __launch_bounds__(128 * kPairs, (HD == 64 ? 4 : 3)) void flash_dkv_pair_kernel(FlashArgs a, int parts) {
   using O = Ops<bf16_t, HD>;
   using S = Stager<bf16_t, HD, 32, kPairs>;
-  constexpr int TILE = 32 * O::ROW, TURNS = 3;
-  __shared__ __align__(16) char lds[TURNS][2][TILE];       // [turn][queries, output gradients]
-  __shared__ __align__(16) float prob[2][kPairs][1024];    // [step's parity][pair]: probabilities in lane order
-  __shared__ __align__(16) float stat[TURNS][2 * kPairs][64];  // [turn][wave]: log-sum-exps, negated deltas
+  constexpr int TILE = 32 * O::ROW;
+  // queries of the step behind, the current and the next one; output gradients of the current and
+  // the next one
+  __shared__ __align__(16) char lds[5][TILE];
+  __shared__ __align__(16) f16x8_v prob[2][kPairs][128];   // [step's parity][pair]: probabilities in lane order
+  __shared__ __align__(16) float stat[2][2 * kPairs][64];  // [step's parity][wave]: log-sum-exps, negated deltas
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool second = wave >= kPairs;
   const int h = lane >> 5, col = lane & 31, pair = second ? wave - kPairs : wave;
@@ -709,9 +730,9 @@ __global__ __launch_bounds__(128 * kPairs, (HD == 64 ? 3 : 2)) void flash_dkv_pa
   const bf16_t* src = head_src;                            // of the next step to load
   const float* src_stat = head_stat;
   int left = w.len - w.first;                              // queries from there on
-  auto load = [&](int t) {
-    stager.load(lds[t][second ? 1 : 0], src, left, pair);
-    load_floats(stat[t][wave], src_stat, left, lane);
+  auto load = [&](int i, int t) {                          // step i, t = i % 3
+    stager.load(lds[second ? 3 + (i & 1) : t], src, left, pair);
+    load_floats(stat[i & 1][wave], src_stat, left, lane);
     src += 32 * ld;
     src_stat += 32;
     left -= 32;
@@ -721,53 +742,56 @@ __global__ __launch_bounds__(128 * kPairs, (HD == 64 ? 3 : 2)) void flash_dkv_pa
       src_stat = head_stat += a.N;
     }
   };
-  load(0);
+  load(0, 0);
   const typename O::Lanes at = O::lanes(lane);
   const float s2 = a.scale * kLog2e;
   f32x16_t acc[HD / 32];
 #pragma unroll
   for (int d = 0; d < HD / 32; ++d) acc[d] = zero16();
-  // what a step begins with: its tiles have arrived everywhere, the next ones are sent for
-  auto begin = [&](int t, int i) {
-    meet();
-    if (i + 1 < total) load((t + 1) % TURNS);
-  };
   int m0 = w.first;                                        // queries of the step at hand
   auto next = [&]() {
     m0 += 32;
     if (m0 >= w.len) m0 = w.first;
   };
+  // A step begins with a meeting: its tiles have arrived everywhere, the next ones are sent for.
   // One step more than there are: the second wave's last.
   if (second) {
-    for (int i = 0, t = 0, b = 0; i <= total; ++i) {
-      begin(t, i);
-      if (i > 0) {
-        if (m0 >= k0) dk_step<HD>(acc, lds[b][0], lds[b][1], stat[b][wave], prob[(i - 1) & 1][pair], at, own, h, lane);
-        next();
-      }
+    f32x16_t dp = zero16();
+    bool before = false;                                   // the step behind has pairs that see each other
+    for (int i = 0, t = 0, b = 2; i <= total; ++i) {
+      const int n = t == 2 ? 0 : t + 1;
+      meet();
+      if (i + 1 < total) load(i + 1, n);
+      if (before) dk_step<HD>(acc, lds[b], prob[(i - 1) & 1][pair], dp, at, lane);
+      before = i < total && m0 >= k0;
+      if (before) dp = dp_step<HD>(lds[3 + (i & 1)], stat[i & 1][wave], at, own, h);
+      next();
       b = t;
-      t = t == TURNS - 1 ? 0 : t + 1;
+      t = n;
     }
   } else {
     for (int i = 0, t = 0; i <= total; ++i) {
-      begin(t, i);
+      const int n = t == 2 ? 0 : t + 1;
+      meet();
       if (i == total) break;
+      if (i + 1 < total) load(i + 1, n);
       if (m0 >= k0)
-        dv_step<HD>(acc, lds[t][0], lds[t][1], stat[t][wave], prob[i & 1][pair], at, own, m0 == k0, col, s2, h, lane);
+        dv_step<HD>(acc, lds[t], lds[3 + (i & 1)], stat[i & 1][wave], prob[i & 1][pair], at, own, m0 == k0, col, s2, h,
+                    lane);
       next();
-      t = t == TURNS - 1 ? 0 : t + 1;
+      t = n;
     }
   }
   meet();                                                  // the tiles' room takes the results
   if (k0 >= w.len) return;
   const int64_t row0 = w.start + k0;
-  const float by = second ? a.scale : 1.f;
+  const float by = (second ? a.scale : 1.f) * (1.f / kProbScale);
   if (parts > 1) {
     float* sums = a.sums + (((int64_t)(second ? parts : 0) + part) * a.N + row0) * a.nkv * HD + kv * HD;
     if (ki < w.len) store_column<HD>(sums + (int64_t)(lane & 31) * a.nkv * HD, acc, by, h);
     return;
   }
-  char* room = lds[0][0] + wave * 32 * O::ROW;
+  char* room = lds[wave];                                  // four waves, five tiles
   if (second)
     store_rows<bf16_t, HD>(room, reinterpret_cast<bf16_t*>(a.dk) + row0 * a.lddk + kv * HD, a.lddk, w.len - k0, acc, by, lane);
   else
@@ -809,7 +833,7 @@ hipError_t run_backward(const FlashArgs& a, hipStream_t st) {
   flash_dq_kernel<T, HD><<<(unsigned)(slots * (int64_t)a.nkv * (group / together)), 64 * kWaves, 0, st>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if constexpr (sizeof(T) == 2 && HD >= 64) {
+  if constexpr (kByPairs<T, HD>) {
     const int parts = flash_parts(a.N, a.n_seqs, a.nq, a.nkv, HD, DT_BF16);
     flash_dkv_pair_kernel<HD><<<(unsigned)(slots_of(a, 32 * kPairs) * (int64_t)a.nkv * parts), 128 * kPairs, 0, st>>>(
         a, parts);
@@ -828,13 +852,15 @@ hipError_t run_backward(const FlashArgs& a, hipStream_t st) {
 
 int flash_parts(int N, int n_seqs, int nq, int nkv, int hd, int dtype) {
   if (n_seqs < 1) return 1;
-  // Two workgroups of 64 keys fit a compute unit, and tiles differ in work by as much as their
-  // sequence is long.  Below half of the device, and of long sequences below two rounds of it, every
-  // head of the group is a part of its own: one sequence of 8703, 16 heads of 64 on 4, 769 us
-  // in tiles, 375 and 13 for the sums in parts.  Of short ones the sums cost more than the
-  // evenness gains: 64 sequences of at most 200, 32 heads of 128 on 8, 135 us whole, 258 in parts.
+  // Tiles of 64 keys differ in work by as much as their sequence is long.  Below a workgroup per
+  // compute unit, and of long sequences below two rounds of those that fit the device together
+  // (three to a compute unit of heads of 128, four of 64), every head of the group is a part of
+  // its own.  Backward pass whole and in parts: one sequence of 32768, 16 heads of 64 on 4, 8.26 and
+  // 7.35 ms; four of 4096 720 and 562 us; 16 of 2304 762 and 779; three of 2048, 32 heads of 128 on
+  // 8, 489 and 430.  Of short ones the sums cost more than the evenness gains: 24 of 1200, heads
+  // of 64, 362 and 406; six of 1100, heads of 128, 276 and 308.
   const int64_t tiles = ((int64_t)N / 64 + n_seqs / 2) * nkv;
-  const bool cut = tiles < 256 || (tiles < 1024 && N / n_seqs >= 1024);
+  const bool cut = tiles < 256 || (tiles <= (hd == 64 ? 2048 : 1024) && N / n_seqs >= 2048);
   return dtype == DT_BF16 && hd >= 64 && cut ? nq / nkv : 1;
 }
 
