@@ -412,7 +412,8 @@ tandem_status tandem_qk_norm_rope_backward(const tandem_qk_cfg* cfg, const void*
  * no access leaves the arrays; empty sequences are allowed); rows before
  * offsets[0] and from offsets[n_seqs] on belong to no sequence and their
  * outputs are left as they are.  bf16 inputs: products on the matrix cores
- * with float32 sums, probabilities rounded to bf16 for the value product.
+ * with float32 sums, probabilities (backward: score gradients too) rounded to
+ * bf16 for the products that take them.
  * The inputs must be finite: a NaN or infinity in a row of v, in the backward
  * pass of any input, may reach other rows of the same sequence, never another
  * sequence.
