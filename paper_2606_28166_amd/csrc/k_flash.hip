@@ -16,6 +16,8 @@
 // dQ and dK/dV are separate passes: each output is summed by one wave in a fixed
 // order (no atomics), for 7 products where one pass would take 5.
 // float32 models run the same code on the float32 matrix instructions.
+#include <algorithm>
+
 #include "common.h"
 #include "update.h"
 
@@ -525,6 +527,26 @@ __global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_dq_kerne
                     a.lddq, w.len - q0, dq, a.scale, lane);
 }
 
+// A lane's column of a result, float32, 16 bytes at a time.
+template <int HD>
+__device__ __forceinline__ void store_column(float* p, const f32x16_t* acc, float by, int h) {
+#pragma unroll
+  for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      store4(p + 32 * d + 8 * j + 4 * h, acc[d][4 * j] * by, acc[d][4 * j + 1] * by, acc[d][4 * j + 2] * by,
+             acc[d][4 * j + 3] * by);
+}
+
+// One of the even parts of a list, of 2^25 steps and 16 parts at most.
+struct Share {
+  int begin, count;
+};
+__device__ __forceinline__ Share share_of(int all, int part, int parts) {
+  const int begin = (int)((uint32_t)(all * part) / (uint32_t)parts);
+  return Share{begin, (int)((uint32_t)(all * (part + 1)) / (uint32_t)parts) - begin};
+}
+
 template <typename T, int HD>
 __device__ __forceinline__ void dkv_tile(f32x16_t* dk, f32x16_t* dv, const char* __restrict__ tq,
                                          const char* __restrict__ tg, const float* __restrict__ t_lse2,
@@ -555,7 +577,7 @@ __device__ __forceinline__ void dkv_tile(f32x16_t* dk, f32x16_t* dv, const char*
 }
 
 template <typename T, int HD>
-__global__ __launch_bounds__(64 * kWaves, 1) void flash_dkv_kernel(FlashArgs a) {
+__global__ __launch_bounds__(64 * kWaves, 1) void flash_dkv_kernel(FlashArgs a, int parts) {
   using O = Ops<T, HD>;
   constexpr int PER = 32 * kWaves, TILE = kRows * O::ROW;
   // a query past the sequence reads as 0, with log-sum-exp 0: probability 1 of a gradient of 0
@@ -564,10 +586,14 @@ __global__ __launch_bounds__(64 * kWaves, 1) void flash_dkv_kernel(FlashArgs a) 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = lane >> 5, col = lane & 31;
   const int group = a.nq / a.nkv;
-  const int kv = blockIdx.x % a.nkv, slot = blockIdx.x / a.nkv;
+  const int kv = blockIdx.x % a.nkv, part = blockIdx.x / a.nkv % parts, slot = blockIdx.x / a.nkv / parts;
   const Span w = find_span(a.offs, a.n_seqs, a.N, slot, PER, false);
   if (w.first >= w.len) return;
   const int k0 = w.first + 32 * wave, ki = k0 + col;
+  // the heads' tiles of queries, one after the other, and of those this part's
+  const int tiles = (w.len - w.first + kRows - 1) / kRows;
+  const Share mine = share_of(group * tiles, part, parts);
+  int m0 = w.first + mine.begin % tiles * kRows, head = kv * group + mine.begin / tiles;
   const int64_t row = w.start + min(ki, w.len - 1);
   const Stager<T, HD> sq(a.ldq, lane, wave), sg(a.lddo, lane, wave);
   auto load = [&](int t, int head, int m0) {
@@ -578,7 +604,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void flash_dkv_kernel(FlashArgs a) 
     if (wave == 0) load_floats(stat[t][0], a.lse2 + at, w.len - m0, lane);
     if (wave == 1) load_floats(stat[t][1], a.ndelta + at, w.len - m0, lane);
   };
-  load(0, kv * group, w.first);
+  if (mine.count > 0) load(0, head, m0);
   typename O::Right k, v;
   O::load_right(k, reinterpret_cast<const T*>(a.k) + row * a.ldk + kv * HD, h);
   O::load_right(v, reinterpret_cast<const T*>(a.v) + row * a.ldv + kv * HD, h);
@@ -586,9 +612,6 @@ __global__ __launch_bounds__(64 * kWaves, 1) void flash_dkv_kernel(FlashArgs a) 
   f32x16_t dk[HD / 32], dv[HD / 32];
 #pragma unroll
   for (int d = 0; d < HD / 32; ++d) dk[d] = dv[d] = zero16();
-  // the heads' tiles of queries, one after the other
-  const int tiles = (w.len - w.first + kRows - 1) / kRows;
-  int m0 = w.first, head = kv * group;
   const typename O::Lanes at = O::lanes(lane);
   auto step = [&](auto turn, bool more) {
     constexpr int t = decltype(turn)::value;
@@ -600,15 +623,22 @@ __global__ __launch_bounds__(64 * kWaves, 1) void flash_dkv_kernel(FlashArgs a) 
     m0 = m1;
     head = head1;
   };
-  const int total = group * tiles;
-  for (int i = 0; i < total; i += 2) {
-    step(Turn<0>{}, i + 1 < total);
-    if (i + 1 < total) step(Turn<1>{}, i + 2 < total);
+  for (int i = 0; i < mine.count; i += 2) {
+    step(Turn<0>{}, i + 1 < mine.count);
+    if (i + 1 < mine.count) step(Turn<1>{}, i + 2 < mine.count);
   }
   meet();                                                  // the tiles' room takes the results
   if (k0 >= w.len) return;
-  char* room = lds[0][0] + wave * 32 * O::ROW;
   const int64_t row0 = w.start + k0;
+  if (parts > 1) {
+    if (ki >= w.len) return;
+    const int64_t width = a.nkv * HD, plane = (int64_t)parts * a.N * width;
+    float* sums = a.sums + ((int64_t)part * a.N + row0 + col) * width + kv * HD;
+    store_column<HD>(sums, dv, 1.f, h);
+    store_column<HD>(sums + plane, dk, a.scale, h);
+    return;
+  }
+  char* room = lds[0][0] + wave * 32 * O::ROW;
   store_rows<T, HD>(room, reinterpret_cast<T*>(a.dk) + row0 * a.lddk + kv * HD, a.lddk, w.len - k0, dk, a.scale, lane);
   store_rows<T, HD>(room, reinterpret_cast<T*>(a.dv) + row0 * a.lddv + kv * HD, a.lddv, w.len - k0, dv, 1.f, lane);
 }
@@ -667,17 +697,6 @@ __device__ __forceinline__ void dk_step(f32x16_t* dk, const char* __restrict__ t
   O::transposed(dk, tq, at, 0, O::pack(ds));
 }
 
-// A lane's column of a result, float32, 16 bytes at a time.
-template <int HD>
-__device__ __forceinline__ void store_column(float* p, const f32x16_t* acc, float by, int h) {
-#pragma unroll
-  for (int d = 0; d < HD / 32; ++d)
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      store4(p + 32 * d + 8 * j + 4 * h, acc[d][4 * j] * by, acc[d][4 * j + 1] * by, acc[d][4 * j + 2] * by,
-             acc[d][4 * j + 3] * by);
-}
-
 // dK and dV of bf16 heads of 64 and 128 by pairs of waves: of each pair's 32 keys one wave
 // forms the probabilities and dV, the other dP and dK.  Each then holds one operand and one
 // accumulator: three waves of heads of 128 fit a SIMD, four of 64, where one wave with both
@@ -693,8 +712,8 @@ __device__ __forceinline__ void store_column(float* p, const f32x16_t* acc, floa
 // meeting, 676 and 383; four pairs to a workgroup 645 (90 us for the backward pass of 200
 // sequences of at most 30, now 60), six 690.
 //
-// Where the tiles of keys are few, a workgroup takes one part of the group's heads and
-// writes float32 sums, which flash_join_kernel adds up.
+// Where the tiles of keys are few, a workgroup takes one part of the steps and writes float32
+// sums, which flash_join_kernel adds up.
 constexpr int kPairs = 2;
 
 template <int HD>
@@ -711,7 +730,7 @@ __global__ __launch_bounds__(128 * kPairs, (HD == 64 ? 4 : 3)) void flash_dkv_pa
   const bool second = wave >= kPairs;
   const int h = lane >> 5, col = lane & 31, pair = second ? wave - kPairs : wave;
   const int kv = blockIdx.x % a.nkv, part = blockIdx.x / a.nkv % parts, slot = blockIdx.x / a.nkv / parts;
-  const int group = a.nq / a.nkv / parts, head0 = kv * group * parts + part * group;
+  const int group = a.nq / a.nkv;
   const Span w = find_span(a.offs, a.n_seqs, a.N, slot, 32 * kPairs, false);
   if (w.first >= w.len) return;
   const int k0 = w.first + 32 * pair, ki = k0 + col;
@@ -722,14 +741,16 @@ __global__ __launch_bounds__(128 * kPairs, (HD == 64 ? 4 : 3)) void flash_dkv_pa
                             : reinterpret_cast<const bf16_t*>(a.k) + row * a.ldk + kv * HD, h);
   const int64_t ld = second ? a.lddo : a.ldq;
   const S stager(ld, lane, pair);
-  // a step is 32 queries of one head; the heads of the part one after the other
-  const int steps = (w.len - w.first + 31) / 32, total = group * steps;
+  // a step is 32 queries of one head; the heads one after the other, and of those steps this part's
+  const int steps = (w.len - w.first + 31) / 32;
+  const Share mine = share_of(group * steps, part, parts);
+  const int total = mine.count, head0 = kv * group + mine.begin / steps, ahead = mine.begin % steps * 32;
   const bf16_t* head_src = reinterpret_cast<const bf16_t*>(second ? a.dout : a.q) +
                            (int64_t)(w.start + w.first) * ld + head0 * HD;
   const float* head_stat = (second ? a.ndelta : a.lse2) + (int64_t)head0 * a.N + w.start + w.first;
-  const bf16_t* src = head_src;                            // of the next step to load
-  const float* src_stat = head_stat;
-  int left = w.len - w.first;                              // queries from there on
+  const bf16_t* src = head_src + ahead * ld;               // of the next step to load
+  const float* src_stat = head_stat + ahead;
+  int left = w.len - w.first - ahead;                      // queries from there on
   auto load = [&](int i, int t) {                          // step i, t = i % 3
     stager.load(lds[second ? 3 + (i & 1) : t], src, left, pair);
     load_floats(stat[i & 1][wave], src_stat, left, lane);
@@ -742,13 +763,13 @@ __global__ __launch_bounds__(128 * kPairs, (HD == 64 ? 4 : 3)) void flash_dkv_pa
       src_stat = head_stat += a.N;
     }
   };
-  load(0, 0);
+  if (total > 0) load(0, 0);
   const typename O::Lanes at = O::lanes(lane);
   const float s2 = a.scale * kLog2e;
   f32x16_t acc[HD / 32];
 #pragma unroll
   for (int d = 0; d < HD / 32; ++d) acc[d] = zero16();
-  int m0 = w.first;                                        // queries of the step at hand
+  int m0 = w.first + ahead;                                // queries of the step at hand
   auto next = [&]() {
     m0 += 32;
     if (m0 >= w.len) m0 = w.first;
@@ -800,6 +821,7 @@ __global__ __launch_bounds__(128 * kPairs, (HD == 64 ? 4 : 3)) void flash_dkv_pa
 
 // dV (blockIdx.y 0) and dK (1) from the parts' sums, 8 elements per thread; rows of no
 // sequence stay as they are.
+template <typename T>
 __global__ __launch_bounds__(256) void flash_join_kernel(FlashArgs a, int width, int parts) {
   const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8, row = i / width;
   const int c = (int)(i % width);
@@ -811,7 +833,7 @@ __global__ __launch_bounds__(256) void flash_join_kernel(FlashArgs a, int width,
     lo += *reinterpret_cast<const f32x4_t*>(p);
     hi += *reinterpret_cast<const f32x4_t*>(p + 4);
   }
-  bf16_t* out = blockIdx.y ? reinterpret_cast<bf16_t*>(a.dk) + row * a.lddk : reinterpret_cast<bf16_t*>(a.dv) + row * a.lddv;
+  T* out = blockIdx.y ? reinterpret_cast<T*>(a.dk) + row * a.lddk : reinterpret_cast<T*>(a.dv) + row * a.lddv;
   store4(out + c, lo[0], lo[1], lo[2], lo[3]);
   store4(out + c + 4, hi[0], hi[1], hi[2], hi[3]);
 }
@@ -833,18 +855,18 @@ hipError_t run_backward(const FlashArgs& a, hipStream_t st) {
   flash_dq_kernel<T, HD><<<(unsigned)(slots * (int64_t)a.nkv * (group / together)), 64 * kWaves, 0, st>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if constexpr (kByPairs<T, HD>) {
-    const int parts = flash_parts(a.N, a.n_seqs, a.nq, a.nkv, HD, DT_BF16);
-    flash_dkv_pair_kernel<HD><<<(unsigned)(slots_of(a, 32 * kPairs) * (int64_t)a.nkv * parts), 128 * kPairs, 0, st>>>(
-        a, parts);
-    if (parts > 1) {
-      const hipError_t f = hipGetLastError();
-      if (f != hipSuccess) return f;
-      const int width = a.nkv * HD;
-      flash_join_kernel<<<dim3((unsigned)(((int64_t)a.N * width / 8 + 255) / 256), 2), 256, 0, st>>>(a, width, parts);
-    }
-  } else
-    flash_dkv_kernel<T, HD><<<(unsigned)(slots_of(a, 32 * kWaves) * (int64_t)a.nkv), 64 * kWaves, 0, st>>>(a);
+  const int parts = flash_parts(a.N, a.n_seqs, a.nq, a.nkv, HD, sizeof(T) == 2 ? DT_BF16 : DT_F32);
+  const int64_t along = (int64_t)a.nkv * parts;
+  if constexpr (kByPairs<T, HD>)
+    flash_dkv_pair_kernel<HD><<<(unsigned)(slots_of(a, 32 * kPairs) * along), 128 * kPairs, 0, st>>>(a, parts);
+  else
+    flash_dkv_kernel<T, HD><<<(unsigned)(slots_of(a, 32 * kWaves) * along), 64 * kWaves, 0, st>>>(a, parts);
+  if (parts > 1) {
+    const hipError_t f = hipGetLastError();
+    if (f != hipSuccess) return f;
+    const int width = a.nkv * HD;
+    flash_join_kernel<T><<<dim3((unsigned)(((int64_t)a.N * width / 8 + 255) / 256), 2), 256, 0, st>>>(a, width, parts);
+  }
   return hipGetLastError();
 }
 
@@ -852,16 +874,23 @@ hipError_t run_backward(const FlashArgs& a, hipStream_t st) {
 
 int flash_parts(int N, int n_seqs, int nq, int nkv, int hd, int dtype) {
   if (n_seqs < 1) return 1;
-  // Tiles of 64 keys differ in work by as much as their sequence is long.  Below a workgroup per
-  // compute unit, and of long sequences below two rounds of those that fit the device together
-  // (three to a compute unit of heads of 128, four of 64), every head of the group is a part of
-  // its own.  Backward pass whole and in parts: one sequence of 32768, 16 heads of 64 on 4, 8.26 and
-  // 7.35 ms; four of 4096 720 and 562 us; 16 of 2304 762 and 779; three of 2048, 32 heads of 128 on
-  // 8, 489 and 430.  Of short ones the sums cost more than the evenness gains: 24 of 1200, heads
-  // of 64, 362 and 406; six of 1100, heads of 128, 276 and 308.
-  const int64_t tiles = ((int64_t)N / 64 + n_seqs / 2) * nkv;
-  const bool cut = tiles < 256 || (tiles <= (hd == 64 ? 2048 : 1024) && N / n_seqs >= 2048);
-  return dtype == DT_BF16 && hd >= 64 && cut ? nq / nkv : 1;
+  // Tiles of keys (64, or 128 of the other form) differ in work by as much as their sequence is
+  // long.  Below a workgroup per compute unit, and of long sequences below some rounds of those
+  // that fit the device together, they are cut into parts that give `want` workgroups, unless
+  // a part would be shorter than about 8 steps.  Backward pass whole and in parts, us:
+  //   bf16    one sequence of 32768, 16 heads of 64 on 4, 8256 and 7635; four of 4096 720 and 571;
+  //           one of 4000, 8 heads of 128 on 1, 435 and 185; three of 2048, 32 on 8, 489 and 434
+  //   float32 four of at most 7998, 4 heads of 32 on 2, 1598 and 758; one of 2000, 16 heads of 64
+  //           on 4, 1243 and 386
+  // Of short ones the sums cost more than the evenness gains: bf16, 24 of 1200, heads of 64, 362
+  // and 406; six of 1100, heads of 128, 276 and 308; eight of at most 253, 16 heads of 128 on 8, 33
+  // and 49.
+  const bool pairs = dtype == DT_BF16 && hd >= 64;
+  const int64_t tiles = (N / (pairs ? 64 : 128) + n_seqs / 2) * (int64_t)nkv, len = N / n_seqs;
+  const int64_t want = pairs && hd == 64 ? 4096 : 2048;
+  if (tiles >= 256 && (tiles > (pairs ? want / 2 : want) || len < (pairs ? 2048 : 256))) return 1;
+  const int64_t most = std::min<int64_t>(16, len * (nq / nkv) / (pairs ? 256 : 64));
+  return most < 2 ? 1 : (int)std::min(most, std::max<int64_t>(2, (want + tiles) / (tiles + 1)));
 }
 
 int64_t flash_blocks(int N, int n_seqs, int nq, int nkv) {

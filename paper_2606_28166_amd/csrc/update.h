@@ -59,7 +59,7 @@ struct FlashArgs {
   const void* dout; void* dq; void* dk; void* dv;
   int64_t lddo, lddq, lddk, lddv;
   float* ndelta; float* lse2;              // workspace of the backward pass, [nq][N] each
-  float* sums;                             // and [dV, dK][parts][N][nkv][hd], where a group's heads are cut into parts
+  float* sums;                             // and [dV, dK][parts][N][nkv][hd], where the work on a tile is cut into parts
 };
 int flash_parts(int N, int n_seqs, int nq, int nkv, int hd, int dtype);
 int64_t flash_blocks(int N, int n_seqs, int nq, int nkv);  // workgroups of a launch, at most
