@@ -877,7 +877,7 @@ int flash_parts(int N, int n_seqs, int nq, int nkv, int hd, int dtype) {
   // Tiles of keys (64, or 128 of the other form) differ in work by as much as their sequence is
   // long.  Below a workgroup per compute unit, and the longer the sequences below the more rounds
   // of those that fit the device together, they are cut into parts that give `want`
-  // workgroups, unless a part would be shorter than about 8 steps.  Backward pass whole and
+  // workgroups, four at least, unless a part would be shorter than about 8 steps.  Backward pass whole and
   // in parts, us:
   //   bf16    one sequence of 32768, 16 heads of 64 on 4, 8256 and 7635; four of 4096 720 and 571;
   //           three of 2048, 32 of 128 on 8, 489 and 434; 20 of at most 1973, 8 of 64 on 2, 223 and 186
@@ -888,11 +888,11 @@ int flash_parts(int N, int n_seqs, int nq, int nkv, int hd, int dtype) {
   // and 49.
   const bool pairs = dtype == DT_BF16 && hd >= 64;
   const int64_t tiles = (N / (pairs ? 64 : 128) + n_seqs / 2) * (int64_t)nkv, len = N / n_seqs;
-  const int64_t want = pairs && hd == 64 ? 4096 : 2048;
-  const int64_t few = pairs ? std::min(want / 2, want * len / 4096) : std::min(want, want * len / 512);
+  const int64_t want = pairs && hd == 128 ? 1024 : 2048;
+  const int64_t few = std::min(want, want * len / (pairs ? 2048 : 512));
   if (tiles > std::max<int64_t>(256, few)) return 1;
   const int64_t most = std::min<int64_t>(16, len * (nq / nkv) / (pairs ? 256 : 64));
-  return most < 2 ? 1 : (int)std::min(most, std::max<int64_t>(2, (want + tiles) / (tiles + 1)));
+  return most < 2 ? 1 : (int)std::min(most, std::max<int64_t>(4, (want + tiles) / (tiles + 1)));
 }
 
 int64_t flash_blocks(int N, int n_seqs, int nq, int nkv) {
