@@ -558,6 +558,7 @@ class AdamW:
             [(name, {C.c_void_p: np.uint64, C.c_int64: np.int64, C.c_double: np.float64, C.c_int32: np.int32}[t])
              for name, t in L.AdamwTensor._fields_]))
         self._grad_types = self._types
+        self._workspace_bytes = None
 
     def _check_params(self) -> list:
         """The weights' addresses; refuses weights that a step cannot write."""
@@ -604,7 +605,9 @@ class AdamW:
         cfg = L.AdamwCfg(lr, b1, b2, self.eps, self.max_norm, self.steps + 1, self.elems)
         need, norm = 0, None
         if self.max_norm > 0:
-            need = _need(_lib.tandem_adamw_workspace_size, cfg, self._table, len(types))
+            if self._workspace_bytes is None:          # a matter of the weights' sizes
+                self._workspace_bytes = _need(_lib.tandem_adamw_workspace_size, cfg, self._table, len(types))
+            need = self._workspace_bytes
             norm = torch.empty((), dtype=torch.float32, device=self.dev)
         workspace = _workspace(None, need, self.dev)
         _run(self.dev, _lib.tandem_adamw, cfg, self._table, len(types), self.m.data_ptr(), self.v.data_ptr(),
