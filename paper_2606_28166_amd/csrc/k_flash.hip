@@ -692,7 +692,8 @@ __device__ __forceinline__ void dk_step(f32x16_t* dk, const char* __restrict__ t
   for (int j = 0; j < 2; ++j) {
     const f16x8_v p = prob[64 * j + lane];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) ds[8 * j + e] = (float)p[e] * dp[8 * j + e];
+    for (int e = 0; e < 8; ++e)              // with the 0 one instruction converts and multiplies: 1% of the time
+      ds[8 * j + e] = __builtin_fmaf((float)p[e], dp[8 * j + e], 0.f);
   }
   O::transposed(dk, tq, at, 0, O::pack(ds));
 }
@@ -707,7 +708,7 @@ __device__ __forceinline__ void dk_step(f32x16_t* dk, const char* __restrict__ t
 // The matrix pipe is busy 50% of the cycles; waves wait at the meetings and for LDS.  What bounds
 // a long run is power: the clock goes down to 1.7 GHz, and a form that took a quarter more
 // cycles ran at 1.9.  Sixteen ragged rollouts, 32 heads of 128 on 8: 585 us; one sequence of
-// 8703, 16 heads of 64 on 4: 354.  With float32 probabilities and both tiles a step longer, so two
+// 8703, 16 heads of 64 on 4: 352 to 363.  With float32 probabilities and both tiles a step longer, so two
 // workgroups to a compute unit, 632 and 359; the second wave in the same step, at a second
 // meeting, 676 and 383; four pairs to a workgroup 645 (90 us for the backward pass of 200
 // sequences of at most 30, now 60), six 690.
