@@ -465,18 +465,20 @@ hipError_t run_grad(const LogprobArgs& a, hipStream_t st) {
 }  // namespace
 
 int logprob_splits(int R, int V, int* chunk) {
-  // Few rows are cut into parts of at least 8192 entries, about 1024 workgroups together: one
-  // compute unit alone reads at some 46 GB/s (four rows of 151936 float32 logits and their
-  // reference, whole: 26 us by 1024 threads each; in parts 7 us, and 3.5 for the join).
-  const int most = V / 8192;
+  // Few rows are cut into parts of at least a pass of 256 threads by 8 entries, about 1024
+  // workgroups together: one compute unit alone reads at some 46 GB/s.  Four rows of 151936
+  // float32 logits and their reference, replayed from a graph: 7.8 us with the join (9.6 in parts
+  // of 8192; whole 26 by 1024 threads each).  A row of fewer than two parts of 8192 stays whole,
+  // which spares the second launch: eight of 8192 6.6 us, in parts 7.1, and 11.3 and 15.6 where
+  // each call is the host's.
   int want = (1024 + R - 1) / (R > 0 ? R : 1);
-  if (want > most) want = most;
-  if (want < 2) {
+  if (want < 2 || V < 2 * 8192) {
     *chunk = V;
     return 1;
   }
+  if (want > V / 2048) want = V / 2048;
   int c = (V + want - 1) / want;
-  c = (c + 2047) / 2048 * 2048;              // whole passes of 256 threads by 8 entries
+  c = (c + 2047) / 2048 * 2048;              // whole passes
   *chunk = c;
   return (V + c - 1) / c;
 }
