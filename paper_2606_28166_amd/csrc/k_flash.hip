@@ -16,6 +16,11 @@
 // dQ and dK/dV are separate passes: each output is summed by one wave in a fixed
 // order (no atomics), for 7 products where one pass would take 5.
 // float32 models run the same code on the float32 matrix instructions.
+//
+// In bf16 models the probabilities and score gradients are rounded to bf16 where the next
+// product takes them (float32 operands run at a sixteenth of the rate), and dout . out takes the
+// output as it was rounded: 1.7e-3 and 1.0e-3 of the norm of dQ and dK, beside the 1.7e-3 of
+// their own rounding.  Scores, sums, maxima and accumulators are float32.
 #include <algorithm>
 
 #include "common.h"
