@@ -245,6 +245,9 @@ __device__ __forceinline__ void meet() {
   asm volatile("" ::: "memory");
 }
 
+// The same of this wave alone.
+__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+
 __device__ __forceinline__ void store4(bf16_t* p, float a, float b, float c, float d) {
   typedef __bf16 bf16x4_v __attribute__((ext_vector_type(4)));
   *reinterpret_cast<bf16x4_v*>(p) = bf16x4_v{(__bf16)a, (__bf16)b, (__bf16)c, (__bf16)d};
@@ -437,28 +440,152 @@ __global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::FWD)) void flash_kernel(F
   if (h == 0 && qi < w.len) a.lse[(int64_t)head * a.N + row] = (st.m2 + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
+// Where there are few tiles of queries, a workgroup's waves share 32 queries of one head and take
+// every fourth tile of keys each, in LDS of their own and so without a meeting; what they
+// have is joined through LDS.
+template <typename T, int HD>
+struct Alone {
+  using O = Ops<T, HD>;
+  static constexpr int TILE = 32 * O::ROW;
+  // 64 KB at most for four waves' tiles of keys and values, so two workgroups to a compute unit: one
+  // sequence of 4000, 8 heads of 128 on 1, 53 us; two in turn and one workgroup 81
+  static constexpr int TURNS = TILE <= 4096 ? 2 : 1;
+  static constexpr int PART = 32 * HD * 4;                 // bytes of a wave's accumulator
+  typedef char Room[kWaves][TURNS][2][TILE];
+  static_assert(sizeof(Room) >= kWaves * PART && PART >= TILE, "room for the accumulators and the results");
+  struct Work {                                            // of this workgroup
+    Span w;
+    int kv, head;
+  };
+  __device__ __forceinline__ static Work work(const FlashArgs& a) {
+    const int group = a.nq / a.nkv, kv = blockIdx.x % a.nkv;
+    return Work{find_span(a.offs, a.n_seqs, a.N, blockIdx.x / a.nq, 32, true), kv,
+                kv * group + (int)(blockIdx.x / a.nkv) % group};
+  }
+  // use(keys, values, first key) for this wave's tiles of the keys that the queries see
+  template <typename F>
+  __device__ __forceinline__ static void tiles(Room& lds, const FlashArgs& a, const Work& x, int lane, int wave, F&& use) {
+    const T* kb = reinterpret_cast<const T*>(a.k) + (int64_t)(x.w.start + 32 * wave) * a.ldk + x.kv * HD;
+    const T* vb = reinterpret_cast<const T*>(a.v) + (int64_t)(x.w.start + 32 * wave) * a.ldv + x.kv * HD;
+    const Stager<T, HD, 32, 1> sk(a.ldk, lane, 0), sv(a.ldv, lane, 0);
+    auto load = [&](int t, int n0) {
+      sk.load(lds[wave][t][0], kb, x.w.len - n0, 0);
+      sv.load(lds[wave][t][1], vb, x.w.len - n0, 0);
+      kb += 32 * kWaves * a.ldk;
+      vb += 32 * kWaves * a.ldv;
+    };
+    int t = 0;
+    if (TURNS == 2 && 32 * wave <= x.w.first) load(0, 32 * wave);
+    for (int n0 = 32 * wave; n0 <= x.w.first; n0 += 32 * kWaves) {
+      if (TURNS == 1) {
+        arrived();                                         // the last tile has been read
+        load(0, n0);
+      }
+      arrived();
+      if (TURNS == 2 && n0 + 32 * kWaves <= x.w.first) load(t ^ 1, n0 + 32 * kWaves);
+      use(lds[wave][t][0], lds[wave][t][1], n0);
+      if (TURNS == 2) t ^= 1;
+    }
+  }
+  // The waves' accumulators, each times its f, added up in the first wave's, in their order.
+  __device__ __forceinline__ static void join(Room& lds, f32x16_t* acc, float f, int lane, int wave) {
+    char* room = lds[0][0][0];
+    f32x4_t* own = reinterpret_cast<f32x4_t*>(room + wave * PART) + lane;
+    if (wave > 0) {
+#pragma unroll
+      for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          own[64 * (4 * d + j)] =
+              f32x4_t{acc[d][4 * j] * f, acc[d][4 * j + 1] * f, acc[d][4 * j + 2] * f, acc[d][4 * j + 3] * f};
+    }
+    meet();
+    if (wave > 0) return;
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d) acc[d] *= f;
+    for (int o = 1; o < kWaves; ++o) {
+      const f32x4_t* part = reinterpret_cast<const f32x4_t*>(room + o * PART) + lane;
+#pragma unroll
+      for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const f32x4_t v = part[64 * (4 * d + j)];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[d][4 * j + e] += v[e];
+        }
+    }
+  }
+};
+
+template <typename T, int HD>
+__global__ __launch_bounds__(64 * kWaves, 2) void flash_alone_kernel(FlashArgs a) {
+  using O = Ops<T, HD>;
+  using A = Alone<T, HD>;
+  __shared__ __align__(16) typename A::Room lds;
+  __shared__ float stat[kWaves][2][32];                    // maxima, sums
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = lane >> 5, col = lane & 31;
+  const typename A::Work x = A::work(a);
+  if (x.w.first >= x.w.len) return;
+  const int q0 = x.w.first, qi = q0 + col;
+  const int64_t row = x.w.start + min(qi, x.w.len - 1);
+  typename O::Right q;
+  O::load_right(q, reinterpret_cast<const T*>(a.q) + row * a.ldq + x.head * HD, h);
+  const float s2 = a.scale * kLog2e;
+  const typename O::Lanes at = O::lanes(lane);
+  Softmax<T, HD> st;
+#pragma unroll
+  for (int d = 0; d < HD / 32; ++d) st.o[d] = zero16();
+  A::tiles(lds, a, x, lane, wave, [&](const char* __restrict__ tk, const char* __restrict__ tv, int n0) {
+    st.add(tk, tv, at, q, n0, q0, qi, s2, h);
+  });
+  const float own = st.l + __shfl_xor(st.l, 32, kWave);
+  if (h == 0) {
+    stat[wave][0][col] = st.m2;
+    stat[wave][1][col] = own;
+  }
+  meet();                                                  // the tiles' room takes the accumulators
+  float m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int o = 0; o < kWaves; ++o) m = fmaxf(m, stat[o][0][col]);
+#pragma unroll
+  for (int o = 0; o < kWaves; ++o) l += stat[o][1][col] * __builtin_amdgcn_exp2f(stat[o][0][col] - m);
+  A::join(lds, st.o, __builtin_amdgcn_exp2f(st.m2 - m), lane, wave);
+  if (wave > 0) return;
+  store_rows<T, HD>(lds[0][0][0], reinterpret_cast<T*>(a.out) + (int64_t)(x.w.start + q0) * a.ldo + x.head * HD, a.ldo,
+                    x.w.len - q0, st.o, 1.f / l, lane);
+  if (h == 0 && qi < x.w.len) a.lse[(int64_t)x.head * a.N + row] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// A block of 32 keys, the first at n0: the tile's rows from r0 on.
+template <typename T, int HD>
+__device__ __forceinline__ void dq_block(f32x16_t* dq, const char* __restrict__ tk, const char* __restrict__ tv, int r0,
+                                         const typename Ops<T, HD>::Lanes& at, const typename Ops<T, HD>::Right& q,
+                                         const typename Ops<T, HD>::Right& g, int n0, bool edge, int qi, float s2,
+                                         float lse2, float delta, int h) {
+  using O = Ops<T, HD>;
+  const f32x16_t s = O::by_rows(tk, at, r0, q);
+  const f32x16_t dp = O::by_rows(tv, at, r0, g);
+  float ds[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    ds[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], s2, -lse2)) * (dp[i] - delta);
+  if (edge) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (n0 + result_row(i, h) > qi) ds[i] = 0.f;
+  }
+  O::transposed(dq, tk, at, r0, O::pack(ds));
+}
 template <typename T, int HD>
 __device__ __forceinline__ void dq_tile(f32x16_t* dq, const char* __restrict__ tk, const char* __restrict__ tv,
                                         const typename Ops<T, HD>::Lanes& at, const typename Ops<T, HD>::Right& q,
                                         const typename Ops<T, HD>::Right& g, int n0, int q0, int qi, float s2,
                                         float lse2, float delta, int h) {
-  using O = Ops<T, HD>;
   const bool edge = n0 + kRows - 1 > q0;
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
-    const f32x16_t s = O::by_rows(tk, at, 32 * b, q);
-    const f32x16_t dp = O::by_rows(tv, at, 32 * b, g);
-    float ds[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      ds[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], s2, -lse2)) * (dp[i] - delta);
-    if (edge) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (n0 + 32 * b + result_row(i, h) > qi) ds[i] = 0.f;
-    }
-    O::transposed(dq, tk, at, 32 * b, O::pack(ds));
-  }
+  for (int b = 0; b < 2; ++b)
+    dq_block<T, HD>(dq, tk, tv, 32 * b, at, q, g, n0 + 32 * b, edge, qi, s2, lse2, delta, h);
 }
 
 // The pairs' probabilities are held as 2^15 P, in float16 where they pass from wave to wave:
@@ -468,8 +595,29 @@ constexpr float kProbScale = 32768.f, kProbBits = 15.f;
 template <typename T, int HD>
 constexpr bool kByPairs = sizeof(T) == 2 && HD >= 64;     // dK and dV by pairs of waves
 
-// dQ, and for the pass over the keys the deltas dout . out (negated) and the log-sum-exps in
-// powers of two, each (row, head) being one lane pair's.
+// What a lane holds of its query, and leaves for the pass over the keys (if `leave`): the delta
+// dout . out (negated) and the log-sum-exp in powers of two.
+template <typename T, int HD>
+struct DqRows {
+  using O = Ops<T, HD>;
+  typename O::Right q, g;
+  float delta, lse2;
+  __device__ __forceinline__ DqRows(const FlashArgs& a, int head, int64_t row, int h, bool leave) {
+    O::load_right(g, reinterpret_cast<const T*>(a.dout) + row * a.lddo + head * HD, h);
+    O::load_right(q, reinterpret_cast<const T*>(a.out) + row * a.ldo + head * HD, h);
+    delta = O::dot(g, q);
+    delta += __shfl_xor(delta, 32, kWave);
+    O::load_right(q, reinterpret_cast<const T*>(a.q) + row * a.ldq + head * HD, h);
+    const int64_t stat = (int64_t)head * a.N + row;
+    lse2 = a.lse[stat] * kLog2e;
+    if (h == 0 && leave) {
+      a.ndelta[stat] = -delta;
+      a.lse2[stat] = kByPairs<T, HD> ? lse2 - kProbBits : lse2;
+    }
+  }
+};
+
+// dQ, and what the pass over the keys needs, each (row, head) being one lane pair's.
 // The matrix pipe is busy 50% (heads of 128) and 65% (64) of the cycles: sixteen ragged rollouts
 // 392 to 420 us as the clock allows, one sequence of 8703 235.  Two waves a SIMD; tiles of 32
 // keys, or four waves a SIMD of heads of 64, take the same time.
@@ -499,18 +647,7 @@ __global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_dq_kerne
     vb += dv;
   };
   load(0, 0);
-  typename O::Right q, g;
-  O::load_right(g, reinterpret_cast<const T*>(a.dout) + row * a.lddo + head * HD, h);
-  O::load_right(q, reinterpret_cast<const T*>(a.out) + row * a.ldo + head * HD, h);
-  float delta = O::dot(g, q);
-  delta += __shfl_xor(delta, 32, kWave);
-  O::load_right(q, reinterpret_cast<const T*>(a.q) + row * a.ldq + head * HD, h);
-  const int64_t stat = (int64_t)head * a.N + row;
-  const float lse2 = a.lse[stat] * kLog2e;
-  if (h == 0 && qi < w.len) {      // for the pass over the keys
-    a.ndelta[stat] = -delta;
-    a.lse2[stat] = kByPairs<T, HD> ? lse2 - kProbBits : lse2;
-  }
+  const DqRows<T, HD> r(a, head, row, h, qi < w.len);
   const float s2 = a.scale * kLog2e;
   f32x16_t dq[HD / 32];
 #pragma unroll
@@ -520,7 +657,7 @@ __global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_dq_kerne
     constexpr int t = decltype(turn)::value;
     meet();
     if (n0 + kRows < end) load(t ^ 1, n0 + kRows);
-    if (n0 <= q0 + 31) dq_tile<T, HD>(dq, lds[t][0], lds[t][1], at, q, g, n0, q0, qi, s2, lse2, delta, h);
+    if (n0 <= q0 + 31) dq_tile<T, HD>(dq, lds[t][0], lds[t][1], at, r.q, r.g, n0, q0, qi, s2, r.lse2, r.delta, h);
   };
   for (int n0 = 0; n0 < end; n0 += 2 * kRows) {
     step(Turn<0>{}, n0);
@@ -530,6 +667,33 @@ __global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_dq_kerne
   if (q0 >= w.len) return;
   store_rows<T, HD>(lds[0][0] + wave * 32 * O::ROW, reinterpret_cast<T*>(a.dq) + (int64_t)(w.start + q0) * a.lddq + head * HD,
                     a.lddq, w.len - q0, dq, a.scale, lane);
+}
+
+template <typename T, int HD>
+__global__ __launch_bounds__(64 * kWaves, 2) void flash_dq_alone_kernel(FlashArgs a) {
+  using O = Ops<T, HD>;
+  using A = Alone<T, HD>;
+  __shared__ __align__(16) typename A::Room lds;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = lane >> 5, col = lane & 31;
+  const typename A::Work x = A::work(a);
+  if (x.w.first >= x.w.len) return;
+  const int q0 = x.w.first, qi = q0 + col;
+  const int64_t row = x.w.start + min(qi, x.w.len - 1);
+  const DqRows<T, HD> r(a, x.head, row, h, wave == 0 && qi < x.w.len);
+  const float s2 = a.scale * kLog2e;
+  f32x16_t dq[HD / 32];
+#pragma unroll
+  for (int d = 0; d < HD / 32; ++d) dq[d] = zero16();
+  const typename O::Lanes at = O::lanes(lane);
+  A::tiles(lds, a, x, lane, wave, [&](const char* __restrict__ tk, const char* __restrict__ tv, int n0) {
+    dq_block<T, HD>(dq, tk, tv, 0, at, r.q, r.g, n0, n0 + 31 > q0, qi, s2, r.lse2, r.delta, h);
+  });
+  meet();                                                  // the tiles' room takes the accumulators
+  A::join(lds, dq, 1.f, lane, wave);
+  if (wave > 0) return;
+  store_rows<T, HD>(lds[0][0][0], reinterpret_cast<T*>(a.dq) + (int64_t)(x.w.start + q0) * a.lddq + x.head * HD, a.lddq,
+                    x.w.len - q0, dq, a.scale, lane);
 }
 
 // A lane's column of a result, float32, 16 bytes at a time.
@@ -846,8 +1010,25 @@ __global__ __launch_bounds__(256) void flash_join_kernel(FlashArgs a, int width,
 
 int slots_of(const FlashArgs& a, int per) { return a.N / per + a.n_seqs; }
 
+// Whether the tiles of queries are so few that the keys are shared out: below two workgroups per
+// compute unit, if there are tiles enough to share (with one tile of a wave in LDS, more).
+// Forward, us: one sequence of 2000, float32, 4 heads of 32 on 2, 79 and shared 27; bf16, one of 8703, 2 heads
+// of 64 on 2, 131 and 46; one of 2000, 16 of 128 on 8, 45 and 36.  Not so few: 64 of at most 1000,
+// float32, 98 and 122; one of 8703, 16 of 64 on 4, 187 and 287.  Short: eight of at most 373, 16 of
+// 128 on 8, 16 and 19; 20 of at most 299, 8 of 64 on 2, backward 36 and 40.
+template <typename T, int HD>
+bool few_queries(const FlashArgs& a) {
+  const int together = heads_together(a.nq / a.nkv);
+  const int64_t workgroups = ((int64_t)a.N * together / (32 * kWaves) + a.n_seqs / 2) * (a.nq / together);
+  return workgroups < 512 && a.N / a.n_seqs >= (Alone<T, HD>::TURNS == 2 ? 160 : 512);
+}
+
 template <typename T, int HD>
 hipError_t run(const FlashArgs& a, hipStream_t st) {
+  if (few_queries<T, HD>(a)) {
+    flash_alone_kernel<T, HD><<<(unsigned)(slots_of(a, 32) * (int64_t)a.nq), 64 * kWaves, 0, st>>>(a);
+    return hipGetLastError();
+  }
   const int group = a.nq / a.nkv, together = heads_together(group);
   const int slots = slots_of(a, 32 * (kWaves / together));
   flash_kernel<T, HD><<<(unsigned)(slots * (int64_t)a.nkv * (group / together)), 64 * kWaves, 0, st>>>(a);
@@ -857,8 +1038,12 @@ hipError_t run(const FlashArgs& a, hipStream_t st) {
 template <typename T, int HD>
 hipError_t run_backward(const FlashArgs& a, hipStream_t st) {
   const int group = a.nq / a.nkv, together = heads_together(group);
-  const int slots = slots_of(a, 32 * (kWaves / together));
-  flash_dq_kernel<T, HD><<<(unsigned)(slots * (int64_t)a.nkv * (group / together)), 64 * kWaves, 0, st>>>(a);
+  if (few_queries<T, HD>(a)) {
+    flash_dq_alone_kernel<T, HD><<<(unsigned)(slots_of(a, 32) * (int64_t)a.nq), 64 * kWaves, 0, st>>>(a);
+  } else {
+    const int slots = slots_of(a, 32 * (kWaves / together));
+    flash_dq_kernel<T, HD><<<(unsigned)(slots * (int64_t)a.nkv * (group / together)), 64 * kWaves, 0, st>>>(a);
+  }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int parts = flash_parts(a.N, a.n_seqs, a.nq, a.nkv, HD, sizeof(T) == 2 ? DT_BF16 : DT_F32);

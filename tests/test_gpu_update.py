@@ -445,6 +445,7 @@ def _attention_inputs(N, nq, nkv, hd, dt, seed):
 LENS = {
     "single": [1], "pair": [1, 2], "empty": [0, 5, 0, 0, 3, 0], "edges": [31, 32, 33, 63, 64, 65, 1],
     "tiles": [127, 128, 129, 0, 191, 257], "many": [(7 * i) % 23 for i in range(150)], "long": [1037],
+    "few": [1100, 0, 1, 1503],
 }
 
 
