@@ -11,7 +11,8 @@ magnitudes:
 * q/k: the angle is reduced in 64 bits and rounded once, 2 pi 2^-25 < 2^-22; sums of
   squares run over 16 products and 3 exchanges; all of it below 2^-20 of |x1| + |x2|.
 * attention: a score carries (hd + 4) u sum |q||k| scale, which is its probability's
-  relative error; bf16 probabilities and score gradients are rounded once more, 2^-8.
+  relative error; bf16 probabilities and score gradients are rounded once more, 2^-8, and
+  the probabilities in the score gradients may be of 11 bits.
 * AdamW: fewer than 32 operations per element.
 """
 import itertools
@@ -386,6 +387,9 @@ def _attention_reference(q, k, v, dout, offs, scale):
     G = nq // nkv
     # a bf16 probability and score gradient is rounded once more; float32 ones are not
     e_p = _half(BF) if dt == BF else 4 * U
+    # the P in dS may pass from wave to wave in float16 (of 2^15 P, so no subnormals that count):
+    # half a step is 2^-11 of it, and (1 + 2^-8)(1 + 2^-11) - 1 <= 2^-8 + 2^-11 + 2^-19
+    e_s = e_p + (2.0 ** -11 + 2.0 ** -19 if dt == BF else 0.0)
     h = _half(dt)
     zero = lambda x: torch.zeros(x.shape, dtype=F64, device=DEV)      # noqa: E731
     ref = {n: zero(x) for n, x in (("out", q), ("dq", q), ("dk", k), ("dv", k))}
@@ -417,7 +421,7 @@ def _attention_reference(q, k, v, dout, offs, scale):
             de = (D.abs() * to).sum(1, keepdim=True) + hd * U * (D * o).abs().sum(1, keepdim=True)
             delta = (D * o).sum(1, keepdim=True)
             ds = p * (dp - delta)
-            eds = p * (edp + de + rel * (dp - delta).abs()) + (e_p + 2 * U) * ds.abs()
+            eds = p * (edp + de + rel * (dp - delta).abs()) + (e_s + 2 * U) * ds.abs()
             more = n * U
             ref["dq"][a:b, i] = ds @ K * scale
             tol["dq"][a:b, i] = (eds + more * ds.abs()) @ K.abs() * scale + h * ref["dq"][a:b, i].abs()
