@@ -326,7 +326,8 @@ tandem_status tandem_grpo_loss_noalloc(const tandem_grpo_cfg* cfg, const float* 
  *   lse_diff[r] = lse[r] - log sum_v e^s'_v
  *   kl[r]       = sum_v p_v (s_v - s'_v) - lse_diff[r] = KL(p || q),
  * p = softmax(s), q = softmax(s'); a score of -inf has p_v = 0 and adds
- * nothing, whatever the reference says there.
+ * nothing, whatever the reference says there.  z + bias is formed in float32 and 1 / T
+ * rounded to it; logp and kl do not lose digits to an offset that a row's scores share.
  * A row whose token lies outside [0, vocab) (padding: -1) is left out: its
  * outputs are 0, its gradient row is 0 and its logits are not read.  A row
  * with a NaN or +inf logit has NaN outputs; one with nothing but -inf has an lse

@@ -21,6 +21,14 @@ typedef float f32x4_e4 __attribute__((ext_vector_type(4), aligned(4)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 
+// What the powers of two bear, in them.  A row's maximum is rounded by half a step: up to kMost
+// that changes the sums by a factor of 2 at most, which their logarithm takes back; from 2^30 on
+// it takes them out of float32's range.  Rows beyond, and those with nothing above -inf, are
+// taken in units of the logits (logit_row).  From kFar on the differences of the two models'
+// logits and their weights are summed in 64 bits alone, since a KL is what is left of their mean
+// after the models' offsets.
+constexpr float kMost = 0x1p24f, kFar = 0x1p10f;
+
 // bf16 pair: element 0 in the low half
 __device__ __forceinline__ float lo16(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi16(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
@@ -131,9 +139,9 @@ template <bool REF> struct Eight {
 };
 
 // Folds 8 entries into the running statistics: some 13 vector operations per logit and its
-// reference, an exponential counting two.
+// reference, an exponential counting two.  `far` is whether a maximum of this wave passes kFar.
 template <bool REF>
-__device__ __forceinline__ void fold(Stats& s, const Eight<REF>& a, float c2) {
+__device__ __forceinline__ void fold(Stats& s, bool& far, const Eight<REF>& a, float c2) {
   float mx = a.x[0], my = a.y[0], lo = fminf(a.x[0], a.y[0]);
 #pragma unroll
   for (int e = 1; e < 8; ++e) {
@@ -147,52 +155,83 @@ __device__ __forceinline__ void fold(Stats& s, const Eight<REF>& a, float c2) {
   my *= c2;
   if (__any(mx > s.m || (REF && my > s.mr))) {             // seldom, but at a row's beginning
     raise<REF>(s, fmaxf(s.m, mx), REF ? fmaxf(s.mr, my) : 0.f);
+    if (REF) far = __any(fmaxf(fabsf(against(s.m)), fabsf(against(s.mr))) > kFar);
   }
   const float m = -against(s.m), n = -against(s.mr);
-  // scores of -inf on either side: an entry of probability 0 adds nothing, whatever they differ by
-  const bool holes = REF && __any(lo == -INFINITY);
-  float l = 0.f, w = 0.f, lr = 0.f;
+  float p[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(a.x[e], c2, m));
+  if (REF) {
+    float lr = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) lr += __builtin_amdgcn_exp2f(__builtin_fmaf(a.y[e], c2, n));
+    s.lr += (double)lr;
+    // scores of -inf on either side: an entry of probability 0 adds nothing, whatever they differ by
+    if (__any(far || lo == -INFINITY)) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        s.l += (double)p[e];
+        s.w += p[e] > 0.f ? (double)p[e] * ((double)a.x[e] - (double)a.y[e]) : (double)p[e];
+      }
+      return;
+    }
+  }
+  float l = 0.f, w = 0.f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(a.x[e], c2, m));
-    l += p;
-    if (REF) {
-      if (!holes) w += p * (a.x[e] - a.y[e]);
-      else w += p > 0.f ? p * (a.x[e] - a.y[e]) : p;
-      lr += __builtin_amdgcn_exp2f(__builtin_fmaf(a.y[e], c2, n));
-    }
+    l += p[e];
+    if (REF) w += p[e] * (a.x[e] - a.y[e]);
   }
   s.l += (double)l;
-  if (REF) {
-    s.w += (double)w;
-    s.lr += (double)lr;
-  }
+  if (REF) s.w += (double)w;
 }
 
-// A row whose largest score is too low for powers of two, or that has none above -inf (the
-// senior's or the reference's): in units of the logits, by one wave.
+// A row (or its reference's) whose largest score the powers of two do not bear, or that has none
+// above -inf: in units of the logits, by one wave.
 template <typename T, bool REF>
-__device__ __forceinline__ void low_row(const LogprobArgs& a, int r, int lane) {
+__device__ __forceinline__ void logit_row(const LogprobArgs& a, int r, int lane) {
   const T* z = reinterpret_cast<const T*>(a.z) + (size_t)r * a.ldz;
   const T* zr = REF ? reinterpret_cast<const T*>(a.zr) + (size_t)r * a.ldr : nullptr;
-  auto at = [&](const T* p, int v, float b) { return ld(p + v) + (v == a.eos ? b : 0.f); };
+  // use() of the row's entries, 8 at a time
+  auto each = [&](auto&& use) {
+    for (int v = 8 * lane; v < a.V; v += 8 * kWave) {
+      Eight<REF> e;
+      if (v + 8 <= a.V) {
+        Row8<T> c, d;
+        c.load(z + v);
+        if (REF) d.load(zr + v);
+        e.take(c, d);
+      } else {
+        e.some(z, zr, v, a.V);
+      }
+      if (a.eos >= 0) e.add(a.eos - v, a.bias, a.bias_r);
+      use(e);
+    }
+  };
   float m = -INFINITY, n = -INFINITY;
-  for (int v = lane; v < a.V; v += kWave) {
-    m = fmaxf(m, at(z, v, a.bias));
-    if (REF) n = fmaxf(n, at(zr, v, a.bias_r));
-  }
+  each([&](const Eight<REF>& e) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      m = fmaxf(m, e.x[i]);
+      if (REF) n = fmaxf(n, e.y[i]);
+    }
+  });
   m = wave_max(m);
   n = wave_max(n);
+  // the differences against the maxima's: their common part would leave 64 bits few digits of the KL
+  const double m0 = (double)against(m), n0 = (double)against(n);
   double l = 0.0, w = 0.0, lr = 0.0;
-  for (int v = lane; v < a.V; v += kWave) {
-    const float x = at(z, v, a.bias), p = expf((x - against(m)) * a.inv_t);
-    l += (double)p;
-    if (REF) {
-      const float y = at(zr, v, a.bias_r);
-      w += p > 0.f ? (double)p * (double)(x - y) : (double)p;
-      lr += (double)expf((y - against(n)) * a.inv_t);
+  each([&](const Eight<REF>& e) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float p = expf((e.x[i] - against(m)) * a.inv_t);
+      l += (double)p;
+      if (REF) {
+        w += p > 0.f ? (double)p * (((double)e.x[i] - m0) - ((double)e.y[i] - n0)) : (double)p;
+        lr += (double)expf((e.y[i] - against(n)) * a.inv_t);
+      }
     }
-  }
+  });
 #pragma unroll
   for (int o = kWave / 2; o > 0; o >>= 1) {
     l += __shfl_xor(l, o, kWave);
@@ -201,31 +240,34 @@ __device__ __forceinline__ void low_row(const LogprobArgs& a, int r, int lane) {
   }
   if (lane != 0) return;
   const int y = a.tok[r];
+  const float zy = ld(z + y) + (y == a.eos ? a.bias : 0.f);
   const double t = (double)a.inv_t, ll = log(l);
-  a.logp[r] = (float)(((double)at(z, y, a.bias) - (double)m) * t - ll);
+  a.logp[r] = (float)(((double)zy - (double)m) * t - ll);
   a.lse[r] = (float)((double)m * t + ll);
   if (REF) {
-    const double diff = ((double)m - (double)n) * t + (ll - log(lr));
-    a.diff[r] = (float)diff;
-    a.kl[r] = (float)(w * t / l - diff);
+    const double sums = ll - log(lr);
+    a.diff[r] = (float)(((double)m - (double)n) * t + sums);
+    a.kl[r] = (float)(w * t / l - sums);
   }
 }
 
 // A row's outputs from its statistics, by one wave.
 template <typename T, bool REF>
 __device__ __forceinline__ void finish(const LogprobArgs& a, int r, const Stats& s, int lane) {
-  if (s.m < -1e30f || (REF && s.mr < -1e30f)) {
-    low_row<T, REF>(a, r, lane);
+  if (!(fabsf(s.m) <= kMost) || (REF && !(fabsf(s.mr) <= kMost))) {
+    logit_row<T, REF>(a, r, lane);
     return;
   }
   if (lane != 0) return;
   const int y = a.tok[r];
   const float zy = ld(reinterpret_cast<const T*>(a.z) + (size_t)r * a.ldz + y) + (y == a.eos ? a.bias : 0.f);
-  const double ln2 = 0.69314718055994530942, ll = log2(s.l);
-  a.logp[r] = (float)((((double)zy * (double)(a.inv_t * kLog2e) - (double)s.m) - ll) * ln2);
-  a.lse[r] = (float)(((double)s.m + ll) * ln2);
+  // the maxima back into nats by the factor that took them out of them, as it was rounded
+  const float c2 = a.inv_t * kLog2e;
+  const double nats = (double)a.inv_t / (double)c2, ll = log(s.l);
+  a.logp[r] = (float)(((double)zy * (double)c2 - (double)s.m) * nats - ll);
+  a.lse[r] = (float)((double)s.m * nats + ll);
   if (REF) {
-    const double diff = (((double)s.m - (double)s.mr) + (ll - log2(s.lr))) * ln2;
+    const double diff = ((double)s.m - (double)s.mr) * nats + (ll - log(s.lr));
     a.diff[r] = (float)diff;
     a.kl[r] = (float)(s.w * (double)a.inv_t / s.l - diff);
   }
@@ -257,6 +299,7 @@ __global__ __launch_bounds__(256) void logprob_kernel(LogprobArgs a) {
   }
   const float c2 = a.inv_t * kLog2e;
   Stats s = no_stats();
+  bool far = false;
   const int v0 = blockIdx.y * a.chunk, v1 = min(a.V, v0 + a.chunk);
   const T* z = reinterpret_cast<const T*>(a.z) + (size_t)r * a.ldz;
   const T* zr = REF ? reinterpret_cast<const T*>(a.zr) + (size_t)r * a.ldr : nullptr;
@@ -274,13 +317,13 @@ __global__ __launch_bounds__(256) void logprob_kernel(LogprobArgs a) {
       if (REF) d.load(zr + v + 8 * NT);
     }
     if (a.eos >= 0) e.add(a.eos - v, a.bias, a.bias_r);
-    fold<REF>(s, e, c2);
+    fold<REF>(s, far, e, c2);
   }
   if (v < v1) {
     Eight<REF> e;
     e.some(z, zr, v, v1);
     if (a.eos >= 0) e.add(a.eos - v, a.bias, a.bias_r);
-    fold<REF>(s, e, c2);
+    fold<REF>(s, far, e, c2);
   }
   s = wave_merge<REF>(s);
   if (NT > kWave) {
