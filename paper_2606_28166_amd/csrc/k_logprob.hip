@@ -7,7 +7,8 @@
 // lse - lse' = (m - m') + log l - log l' and KL = w / l - (lse - lse').  The maxima are kept
 // in powers of two, rounded once, and everything is taken against the rounded numbers; the
 // differences are formed in 64 bits, once a row, so that a small KL keeps its digits.
-// Backward: p = e^(s - lse) again, elementwise.
+// Backward: p = e^(s - lse) again, elementwise; rows whose lse is so large that its own rounding
+// counts are summed anew.
 // Logits are converted to float32 as they are read.
 #include "common.h"
 #include "update.h"
@@ -365,13 +366,19 @@ __global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a) {
 // one 25 us, 4.6 TB/s.
 constexpr int kGradChunk = 8192;
 
+// Up to what log-sum-exp, and mean difference of the two models' scores, a row's gradient takes
+// them as they were rounded: half a step of lse is an error of p, here an eighth of the
+// result's own rounding in bf16, 2^-17 in float32.
+template <typename T> constexpr float kGradMost = sizeof(T) == 2 ? 4096.f : 256.f;
+
 // What a row's gradient is made of: dz_v = p (A + B (z_v - z'_v)), and `at` more at the token.
 struct RowGrad {
-  float A, B, at, lse2, c2;
+  float A, B, at, lse, inv_t;
 };
 template <bool KL>
 __device__ __forceinline__ float grad_of(const RowGrad& g, float x, float y) {
-  const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x, g.c2, -g.lse2));
+  // the difference first: what is rounded after it is of its size, not of the log-sum-exp's
+  const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x, g.inv_t, -g.lse) * kLog2e);
   // an entry of probability 0 has no gradient, whatever the scores differ by
   return KL ? (p > 0.f ? p * __builtin_fmaf(g.B, x - y, g.A) : p) : p * g.A;
 }
@@ -420,36 +427,86 @@ __device__ __forceinline__ void grad_chunk(const LogprobArgs& a, const RowGrad& 
   }
 }
 
-// The same where the log-sum-exp is too low to be told from the maximum (or there is none):
-// the row's maximum and sum anew, in units of the logits.  One workgroup takes the whole row:
-// the gradient may take the logits' place.
-template <typename T, bool REF>
-__device__ __forceinline__ void low_grad(const LogprobArgs& a, int r, int y, float g, float k, const T* z, const T* zr,
-                                         T* out) {
-  __shared__ float red[4];
-  __shared__ double sums[4];
-  auto at = [&](const T* p, int v, float b) { return ld(p + v) + (v == a.eos ? b : 0.f); };
-  float m = -INFINITY;
-  for (int v = threadIdx.x; v < a.V; v += 256) m = fmaxf(m, at(z, v, a.bias));
-  m = wave_max(m);
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x / kWave] = m;
-  __syncthreads();
-  m = against(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
-  double l = 0.0;
-  for (int v = threadIdx.x; v < a.V; v += 256) l += (double)expf((at(z, v, a.bias) - m) * a.inv_t);
+__device__ __forceinline__ double workgroup_sum(double v, double* room) {
 #pragma unroll
-  for (int o = kWave / 2; o > 0; o >>= 1) l += __shfl_xor(l, o, kWave);
-  if ((threadIdx.x & 63) == 0) sums[threadIdx.x / kWave] = l;
+  for (int o = kWave / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
+  if ((threadIdx.x & 63) == 0) room[threadIdx.x / kWave] = v;
   __syncthreads();
-  l = (sums[0] + sums[1]) + (sums[2] + sums[3]);
-  const bool kl = REF && k != 0.f;
-  const float shift = kl ? a.diff[r] + a.kl[r] : 0.f;
-  for (int v = threadIdx.x; v < a.V; v += 256) {
-    const float x = at(z, v, a.bias), p = (float)((double)expf((x - m) * a.inv_t) / l);
-    float d = g * ((v == y ? 1.f : 0.f) - p);
-    if (kl && !(p == 0.f)) d += k * p * ((x - at(zr, v, a.bias_r)) * a.inv_t - shift);
-    store1(out + v, d * a.inv_t);
+  return (room[0] + room[1]) + (room[2] + room[3]);
+}
+
+// The same of other rows, and of those without a distribution: maximum, sum and mean difference
+// anew, in units of the logits, and from them dz_v = (g ([v = y] - p) + k p ((s_v - s'_v) - mean)) / T.
+// One workgroup takes the whole row: the gradient may take the logits' place.
+template <typename T, bool KL>
+__device__ __forceinline__ void logit_grad(const LogprobArgs& a, float g, float k, const T* z, const T* zr, T* out,
+                                           int y) {
+  __shared__ float red[2][4];
+  __shared__ double sums[2][4];
+  // use(first entry, entries) of the row, 8 at a time
+  auto each = [&](auto&& use) {
+    for (int v = 8 * (int)threadIdx.x; v < a.V; v += 8 * 256) {
+      Eight<KL> e;
+      if (v + 8 <= a.V) {
+        Row8<T> c, d;
+        c.load(z + v);
+        if (KL) d.load(zr + v);
+        e.take(c, d);
+      } else {
+        e.some(z, zr, v, a.V);
+      }
+      if (a.eos >= 0) e.add(a.eos - v, a.bias, a.bias_r);
+      use(v, e);
+    }
+  };
+  float m = -INFINITY, n = -INFINITY;
+  each([&](int, const Eight<KL>& e) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      m = fmaxf(m, e.x[i]);
+      if (KL) n = fmaxf(n, e.y[i]);
+    }
+  });
+  m = wave_max(m);
+  n = wave_max(n);
+  if ((threadIdx.x & 63) == 0) {
+    red[0][threadIdx.x / kWave] = m;
+    red[1][threadIdx.x / kWave] = n;
   }
+  __syncthreads();
+  m = against(fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3])));
+  n = against(fmaxf(fmaxf(red[1][0], red[1][1]), fmaxf(red[1][2], red[1][3])));
+  // a difference of the models' logits against that of their maxima, which may be far larger
+  auto apart = [&](float x, float y) { return ((double)x - (double)m) - ((double)y - (double)n); };
+  double l = 0.0, w = 0.0;
+  each([&](int, const Eight<KL>& e) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float p = expf((e.x[i] - m) * a.inv_t);
+      l += (double)p;
+      // an entry of probability 0 adds nothing, whatever the scores differ by; nor has it a gradient
+      if (KL) w += p > 0.f ? (double)p * apart(e.x[i], e.y[i]) : (double)p;
+    }
+  });
+  l = workgroup_sum(l, sums[0]);
+  const double mean = KL ? workgroup_sum(w, sums[1]) / l : 0.0, t = (double)a.inv_t;
+  each([&](int v, const Eight<KL>& e) {
+    float r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const double p = (double)expf((e.x[i] - m) * a.inv_t) / l;
+      double d = (double)g * ((v + i == y ? 1.0 : 0.0) - p);
+      if (KL && !(p == 0.0)) d += (double)k * p * (t * (apart(e.x[i], e.y[i]) - mean));
+      r[i] = (float)(d * t);
+    }
+    if (v + 8 <= a.V) {
+      store8(out + v, r);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (v + i < a.V) store1(out + v + i, r[i]);
+    }
+  });
 }
 
 template <typename T, bool REF>
@@ -471,15 +528,21 @@ __global__ __launch_bounds__(256) void logprob_grad_kernel(LogprobArgs a, int pa
   }
   const T* z = reinterpret_cast<const T*>(a.z) + (size_t)r * a.ldz;
   const T* zr = REF ? reinterpret_cast<const T*>(a.zr) + (size_t)r * a.ldr : nullptr;
-  const float at = g * a.inv_t, lse2 = a.lse[r] * kLog2e, c2 = a.inv_t * kLog2e;
-  if (!(lse2 > -1e30f)) {
-    if (part == 0) low_grad<T, REF>(a, r, y, g, k, z, zr, out);
-  } else if (REF && k != 0.f) {
-    const RowGrad q = {a.inv_t * (-g - k * (a.diff[r] + a.kl[r])), a.inv_t * k * a.inv_t, at, lse2, c2};
-    grad_chunk<T, true>(a, q, z, zr, out, y, v0, v1);
-  } else {
-    const RowGrad q = {-at, 0.f, at, lse2, c2};
+  const float at = g * a.inv_t, lse = a.lse[r];
+  const bool near = fabsf(lse) < kGradMost<T>;             // false of a NaN
+  if (REF && k != 0.f) {
+    const float mean = a.diff[r] + a.kl[r];
+    if (near && fabsf(mean) < kGradMost<T>) {
+      const RowGrad q = {a.inv_t * (-g - k * mean), a.inv_t * k * a.inv_t, at, lse, a.inv_t};
+      grad_chunk<T, true>(a, q, z, zr, out, y, v0, v1);
+    } else if (part == 0) {
+      logit_grad<T, true>(a, g, k, z, zr, out, y);
+    }
+  } else if (near) {
+    const RowGrad q = {-at, 0.f, at, lse, a.inv_t};
     grad_chunk<T, false>(a, q, z, nullptr, out, y, v0, v1);
+  } else if (part == 0) {
+    logit_grad<T, false>(a, g, 0.f, z, nullptr, out, y);
   }
 }
 

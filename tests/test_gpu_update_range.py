@@ -18,7 +18,7 @@ import math
 import pytest
 import torch
 
-from tests.test_gpu_update import BF, DEV, F32, F64, U, _gen, _logprob_inputs, _say, _scores64, _within
+from tests.test_gpu_update import BF, F32, F64, U, _half, _logprob_inputs, _say, _scores64, _within
 
 pytestmark = pytest.mark.gpu
 
@@ -106,3 +106,68 @@ def test_logprob_of_large_rows_beside_masked_entries(dt):
                 size = want[n].abs() + 40
                 assert ((r[n] - want[n]).abs() <= 32 * U * size).all(), (n, V, a, b)
                 assert ((r[n] - ref[n]).abs() <= 32 * U * size).all(), (n, V, a, b)
+
+
+# The gradient takes p = e^(s - lse) from the float32 lse, which is off by u |lse|, up to a log-sum-exp (and a
+# mean difference of the models' scores) of this much: an eighth of half a step of bf16, 2^-16 in float32.  Other
+# rows are summed anew.
+GRAD_LIMIT = {BF: 4096.0, F32: 256.0}
+
+
+def _gradient_check(grad, z, zr, tok, gl, gk, T, dt):
+    """grad = (g ([v = y] - p) + k p (d - E d)) / T.  p is off by the argument, 5 u of |s - lse| or |s - m|, the
+    exponential and the sum; where lse is taken, by u |lse|.  The terms carry 4 roundings of their sizes, d - E d
+    where it is formed from lse_diff + kl 4 of each part and what those are off by."""
+    s = _scores64(z, T, -1, 0.0)
+    m, logsum, p = _moments(s)
+    lse, depth = m + logsum, (s - m[:, None]).abs()
+    e_sum = 5 * (p * depth).sum(1) + 12
+    hot = torch.zeros_like(p).scatter_(1, tok.long()[:, None], 1.0)
+    g = gl.to(F64)[:, None]
+    want, size = g * (hot - p), g.abs() * (hot + p)
+    taken = lse.abs() < 1.01 * GRAD_LIMIT[dt]
+    extra, flushed = torch.zeros_like(p), g.abs().expand_as(p).clone()
+    if zr is not None:
+        q = _scores64(zr, T, -1, 0.0)
+        n, logsum_r, pr = _moments(q)
+        d = (s - m[:, None]) - (q - n[:, None])
+        mean = (p * d).sum(1, keepdim=True)
+        away = (d - mean).abs()
+        shift = mean[:, 0] + (m - n)
+        taken &= shift.abs() < 1.01 * GRAD_LIMIT[dt]
+        k = gk.to(F64)[:, None]
+        want = want + k * p * (d - mean)
+        size = size + k.abs() * p * away
+        e_mean = (p * away * (5 * depth + 12)).sum(1)
+        diff = (m - n) + logsum - logsum_r
+        kl = mean[:, 0] - (logsum - logsum_r)
+        parts = 17 * (p * (s - q).abs()).sum(1) + 2 * diff.abs() + 5 * kl.abs() + 4 * shift.abs() + 2 * e_sum + \
+            10 * (pr * (q - n[:, None]).abs()).sum(1) + 24
+        extra = U * k.abs() * p * (e_mean[:, None] + torch.where(taken[:, None], parts[:, None] + 4 * (s - q).abs(),
+                                                                torch.zeros_like(p)))
+        flushed += k.abs() * away
+    rel = U * (5 * depth + 5 * (s - m[:, None] - logsum[:, None]).abs() + 16 + e_sum[:, None] +
+               torch.where(taken, lse.abs(), torch.zeros_like(lse))[:, None])
+    tol = (size * rel + extra + 2.0 ** -126 * flushed) / T + _half(dt) * want.abs() / T + 2.0 ** -126
+    _within(grad, want / T, tol, "grad")
+
+
+@pytest.mark.parametrize("dt", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("R,V", [(5, 1000), (3, 40000)])
+def test_logprob_gradient_of_large_rows(R, V, dt):
+    """The same rows and some near the limit, with and without a reference, also in the logits' place."""
+    from paper_2606_28166_amd import engine as E
+    near = [(1.0, 1.0, 1.0), (100.0, -100.0, 1.0), (230.0, 231.0, 1.0), (-260.0, 1.0, 1.0), (2.0, 2.0, 0.02),
+            (1.0, 300.0, 1.0), (4000.0, 4000.0, 1.0), (-4200.0, 4.0, 1.0), (1e5, 1e5, 1.0), (1.0, 1.0, 1e-4)]
+    for i, (base, base_ref, T) in enumerate(near + ROWS + [(torch.finfo(dt).max, torch.finfo(dt).max, 1.0)]):
+        _say("gradient, large", R, V, dt, base, base_ref, T)
+        z, zr, tok, gl, gk = _inputs(R, V, dt, base, base_ref, i)
+        T64 = 1.0 / float(1.0 / torch.tensor(T, dtype=F32))
+        keep = z.clone()
+        f = E.token_logprob(z, tok, ref=zr, temperature=T)
+        a = E.token_logprob_backward(z, tok, f, gl, g_kl=gk, ref=zr, temperature=T)
+        _gradient_check(a, z, zr, tok, gl, gk, T64, dt)
+        b = E.token_logprob_backward(z, tok, f, gl, temperature=T)
+        _gradient_check(b, z, None, tok, gl, None, T64, dt)
+        assert torch.equal(z, keep)
+        assert torch.equal(E.token_logprob_backward(z, tok, f, gl, g_kl=gk, ref=zr, temperature=T, out=z), a)
