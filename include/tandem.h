@@ -411,8 +411,10 @@ tandem_status tandem_qk_norm_rope_backward(const tandem_qk_cfg* cfg, const void*
  * query head h reading key head h / (n_q / n_kv).  offsets is a device array
  * of n_seqs + 1 non-decreasing int32 in [0, N] (values outside are clamped, so
  * no access leaves the arrays; empty sequences are allowed); rows before
- * offsets[0] and from offsets[n_seqs] on belong to no sequence and their
- * outputs are left as they are.  bf16 inputs: products on the matrix cores
+ * offsets[0] and from offsets[n_seqs] on belong to no sequence, their inputs
+ * are not read and their outputs are left as they are, or become 0 in the outputs that
+ * clear names.  A caller whose next step sums over all rows (the gains' gradients, a
+ * projection's weight gradient) needs 0 there.  A call without sequences writes nothing.  bf16 inputs: products on the matrix cores
  * with float32 sums, probabilities (backward: score gradients too) rounded to
  * bf16 for the products that take them.
  * The inputs must be finite: a NaN or infinity in a row of v, in the backward
@@ -430,7 +432,16 @@ typedef struct {
   float scale;                     /* finite, > 0; 1 / sqrt(head_dim) in the models here */
   int64_t q_stride, k_stride, v_stride, out_stride;         /* elements between rows */
   int64_t dout_stride, dq_stride, dk_stride, dv_stride;     /* ignored by the forward pass */
+  int32_t clear;                   /* sum of TANDEM_CLEAR_*; each call looks at its own outputs */
 } tandem_attention_cfg;
+
+enum {                             /* whose rows of no sequence become 0 */
+  TANDEM_CLEAR_OUT = 1,
+  TANDEM_CLEAR_LSE = 2,
+  TANDEM_CLEAR_DQ = 4,
+  TANDEM_CLEAR_DK = 8,
+  TANDEM_CLEAR_DV = 16
+};
 
 /* Workspace of the backward pass (the forward pass needs none). */
 tandem_status tandem_attention_workspace_size(const tandem_attention_cfg* cfg, size_t* bytes);

@@ -76,7 +76,10 @@ class AttentionCfg(C.Structure):
                 ("head_dim", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float),
                 ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64), ("out_stride", C.c_int64),
                 ("dout_stride", C.c_int64), ("dq_stride", C.c_int64), ("dk_stride", C.c_int64),
-                ("dv_stride", C.c_int64)]
+                ("dv_stride", C.c_int64), ("clear", C.c_int32)]
+
+
+CLEAR_OUT, CLEAR_LSE, CLEAR_DQ, CLEAR_DK, CLEAR_DV = 1, 2, 4, 8, 16
 
 
 class AdamwTensor(C.Structure):

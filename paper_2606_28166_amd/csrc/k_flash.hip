@@ -325,6 +325,48 @@ __device__ __forceinline__ Span find_span(const int32_t* offs, int n_seqs, int N
   return r;
 }
 
+// The rows before the first sequence and behind the last one.
+struct Rest {
+  int before, behind, count;     // rows before; first row behind; rows in all
+  __device__ __forceinline__ explicit Rest(const FlashArgs& a) {
+    before = min(max(a.offs[0], 0), a.N);
+    behind = min(max(a.offs[a.n_seqs], before), a.N);
+    count = before + a.N - behind;
+  }
+  __device__ __forceinline__ int row(int i) const { return i < before ? i : behind + (i - before); }
+};
+// They become 0, by all workgroups of a launch of 256 threads in turn: `width` elements of each, and
+// an entry of stat [heads][N].
+template <typename T>
+__device__ __forceinline__ void clear_rows(const FlashArgs& a, void* out, int64_t ld, int width) {
+  const Rest r(a);
+  for (int i = blockIdx.x; i < r.count; i += gridDim.x) {
+    T* row = reinterpret_cast<T*>(out) + r.row(i) * ld;
+    for (int c = threadIdx.x * (16 / (int)sizeof(T)); c < width; c += 256 * (16 / (int)sizeof(T)))
+      *reinterpret_cast<u32x4_t*>(row + c) = u32x4_t{0, 0, 0, 0};
+  }
+}
+__device__ __forceinline__ void clear_stat(const FlashArgs& a, float* stat) {
+  const Rest r(a);
+  for (int i = blockIdx.x; i < r.count; i += gridDim.x)
+    for (int h = threadIdx.x; h < a.nq; h += 256) stat[(int64_t)h * a.N + r.row(i)] = 0.f;
+}
+// The outputs of the forward pass, and of the two passes of the backward one.
+template <typename T, int HD>
+__device__ __forceinline__ void clear_out(const FlashArgs& a) {
+  if (a.clear & TANDEM_CLEAR_OUT) clear_rows<T>(a, a.out, a.ldo, a.nq * HD);
+  if (a.clear & TANDEM_CLEAR_LSE) clear_stat(a, a.lse);
+}
+template <typename T, int HD>
+__device__ __forceinline__ void clear_dq(const FlashArgs& a) {
+  if (a.clear & TANDEM_CLEAR_DQ) clear_rows<T>(a, a.dq, a.lddq, a.nq * HD);
+}
+template <typename T, int HD>
+__device__ __forceinline__ void clear_dkv(const FlashArgs& a) {
+  if (a.clear & TANDEM_CLEAR_DK) clear_rows<T>(a, a.dk, a.lddk, a.nkv * HD);
+  if (a.clear & TANDEM_CLEAR_DV) clear_rows<T>(a, a.dv, a.lddv, a.nkv * HD);
+}
+
 // Query heads of a key head that share a workgroup (the rest of its waves take other
 // positions): the largest power of two that divides the group, up to the waves.
 __host__ __device__ inline int heads_together(int group) {
@@ -396,6 +438,7 @@ __global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::FWD)) void flash_kernel(F
   const int h = lane >> 5, col = lane & 31;
   const int group = a.nq / a.nkv, together = heads_together(group), per = 32 * (kWaves / together);
   const int kv = blockIdx.x % a.nkv, sub = blockIdx.x / a.nkv % (group / together);
+  clear_out<T, HD>(a);
   // the last tiles of a sequence are its longest: they go first
   const Span w = find_span(a.offs, a.n_seqs, a.N, blockIdx.x / a.nkv / (group / together), per, true);
   if (w.first >= w.len) return;
@@ -523,6 +566,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void flash_alone_kernel(FlashArgs a
   using A = Alone<T, HD>;
   __shared__ __align__(16) typename A::Room lds;
   __shared__ float stat[kWaves][2][32];                    // maxima, sums
+  clear_out<T, HD>(a);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = lane >> 5, col = lane & 31;
   const typename A::Work x = A::work(a);
@@ -630,6 +674,7 @@ __global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_dq_kerne
   const int h = lane >> 5, col = lane & 31;
   const int group = a.nq / a.nkv, together = heads_together(group), per = 32 * (kWaves / together);
   const int kv = blockIdx.x % a.nkv, sub = blockIdx.x / a.nkv % (group / together);
+  clear_dq<T, HD>(a);
   const Span w = find_span(a.offs, a.n_seqs, a.N, blockIdx.x / a.nkv / (group / together), per, true);
   if (w.first >= w.len) return;
   const int head = kv * group + sub * together + wave % together;
@@ -674,6 +719,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void flash_dq_alone_kernel(FlashArg
   using O = Ops<T, HD>;
   using A = Alone<T, HD>;
   __shared__ __align__(16) typename A::Room lds;
+  clear_dq<T, HD>(a);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = lane >> 5, col = lane & 31;
   const typename A::Work x = A::work(a);
@@ -756,6 +802,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void flash_dkv_kernel(FlashArgs a, 
   const int h = lane >> 5, col = lane & 31;
   const int group = a.nq / a.nkv;
   const int kv = blockIdx.x % a.nkv, part = blockIdx.x / a.nkv % parts, slot = blockIdx.x / a.nkv / parts;
+  if (parts == 1) clear_dkv<T, HD>(a);
   const Span w = find_span(a.offs, a.n_seqs, a.N, slot, PER, false);
   if (w.first >= w.len) return;
   const int k0 = w.first + 32 * wave, ki = k0 + col;
@@ -901,6 +948,7 @@ __global__ __launch_bounds__(128 * kPairs, (HD == 64 ? 4 : 3)) void flash_dkv_pa
   const int h = lane >> 5, col = lane & 31, pair = second ? wave - kPairs : wave;
   const int kv = blockIdx.x % a.nkv, part = blockIdx.x / a.nkv % parts, slot = blockIdx.x / a.nkv / parts;
   const int group = a.nq / a.nkv;
+  if (parts == 1) clear_dkv<bf16_t, HD>(a);
   const Span w = find_span(a.offs, a.n_seqs, a.N, slot, 32 * kPairs, false);
   if (w.first >= w.len) return;
   const int k0 = w.first + 32 * pair, ki = k0 + col;
@@ -990,16 +1038,18 @@ __global__ __launch_bounds__(128 * kPairs, (HD == 64 ? 4 : 3)) void flash_dkv_pa
 }
 
 // dV (blockIdx.y 0) and dK (1) from the parts' sums, 8 elements per thread; rows of no
-// sequence stay as they are.
+// sequence stay as they are, or become 0.
 template <typename T>
 __global__ __launch_bounds__(256) void flash_join_kernel(FlashArgs a, int width, int parts) {
   const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8, row = i / width;
   const int c = (int)(i % width);
-  if (row >= a.N || row < a.offs[0] || row >= a.offs[a.n_seqs]) return;
+  if (row >= a.N) return;
+  const bool rest = row < a.offs[0] || row >= a.offs[a.n_seqs];
+  if (rest && !(a.clear & (blockIdx.y ? TANDEM_CLEAR_DK : TANDEM_CLEAR_DV))) return;
   const int64_t plane = (int64_t)a.N * width;
   const float* p = a.sums + (int64_t)blockIdx.y * parts * plane + i;
   f32x4_t lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
-  for (int j = 0; j < parts; ++j, p += plane) {
+  for (int j = 0; !rest && j < parts; ++j, p += plane) {
     lo += *reinterpret_cast<const f32x4_t*>(p);
     hi += *reinterpret_cast<const f32x4_t*>(p + 4);
   }

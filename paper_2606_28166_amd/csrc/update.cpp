@@ -155,6 +155,8 @@ tandem_status attention_check(const char* who, const tandem_attention_cfg* c, bo
   if (c->n_seqs < 0) return refuse(TANDEM_E_SHAPE, "%s: n_seqs must be >= 0", who);
   if (!(c->scale > 0.f) || !std::isfinite(c->scale))
     return refuse(TANDEM_E_ARG, "%s: scale must be finite and > 0", who);
+  if ((uint32_t)c->clear > (TANDEM_CLEAR_OUT | TANDEM_CLEAR_LSE | TANDEM_CLEAR_DQ | TANDEM_CLEAR_DK | TANDEM_CLEAR_DV))
+    return refuse(TANDEM_E_ARG, "%s: clear names outputs that there are not", who);
   const int64_t q = (int64_t)c->n_q_heads * c->head_dim, kv = (int64_t)c->n_kv_heads * c->head_dim;
   const struct { const char* what; int64_t stride, least; } st[] = {
       {"q_stride", c->q_stride, q},       {"k_stride", c->k_stride, kv},   {"v_stride", c->v_stride, kv},
@@ -169,6 +171,7 @@ tandem_status attention_check(const char* who, const tandem_attention_cfg* c, bo
   a->scale = c->scale;
   a->ldq = c->q_stride; a->ldk = c->k_stride; a->ldv = c->v_stride; a->ldo = c->out_stride;
   a->lddo = c->dout_stride; a->lddq = c->dq_stride; a->lddk = c->dk_stride; a->lddv = c->dv_stride;
+  a->clear = c->clear;
   return TANDEM_OK;
 }
 

@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "kernels.h"
+#include "tandem.h"
 
 namespace tandem {
 
@@ -59,6 +60,7 @@ struct FlashArgs {
   const void* dout; void* dq; void* dk; void* dv;
   int64_t lddo, lddq, lddk, lddv;
   float* ndelta; float* lse2;              // workspace of the backward pass, [nq][N] each
+  int clear;                               // TANDEM_CLEAR_*
   float* sums;                             // and [dV, dK][parts][N][nkv][hd], where the work on a tile is cut into parts
 };
 int flash_parts(int N, int n_seqs, int nq, int nkv, int hd, int dtype);

@@ -454,13 +454,17 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets: torch.
     rows offsets[s] .. offsets[s + 1] - 1 (int32 on the device) of q
     [N][n_q][head_dim], k and v [N][n_kv][head_dim] are sequence s.  scale:
     1 / sqrt(head_dim) by default.  Returns out [N][n_q][head_dim] and lse
-    float32 [n_q][N]; rows that belong to no sequence are not written."""
+    float32 [n_q][N]; rows that belong to no sequence are 0 in them, but left as
+    they are in an out that is given."""
     cfg, dt, dev = _attention_cfg("attention", q, k, v, offsets, scale)
+    new = torch.empty if cfg.n_seqs > 0 else torch.zeros          # the library clears beside sequences only
+    cfg.clear = L.CLEAR_LSE
     if out is None:
-        out = torch.empty(q.shape, dtype=dt, device=dev)
+        out = new(q.shape, dtype=dt, device=dev)
+        cfg.clear |= L.CLEAR_OUT
     else:
         cfg.out_stride = _rows("attention", "out", out, dt, q.shape, dev)
-    lse = torch.empty((cfg.n_q_heads, cfg.rows), dtype=torch.float32, device=dev)
+    lse = new((cfg.n_q_heads, cfg.rows), dtype=torch.float32, device=dev)
     _run(dev, _lib.tandem_attention, cfg, q.data_ptr(), k.data_ptr(), v.data_ptr(), offsets.data_ptr(), out.data_ptr(),
          lse.data_ptr())
     return dict(out=out, lse=lse)
@@ -472,23 +476,29 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
                        dv: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """Gradients of attention's q, k and v for the gradient dout of its out
     (tandem_attention_backward).  dq, dk, dv may be given, also as views (the
-    value columns of qk_norm_rope_backward's dqkv).  Returns dq, dk, dv."""
+    value columns of qk_norm_rope_backward's dqkv).  Returns dq, dk, dv; rows that
+    belong to no sequence are 0 in those allocated here, and left as they are in given
+    ones."""
     who = "attention_backward"
     cfg, dt, dev = _attention_cfg(who, q, k, v, offsets, scale)
     qs, ks = q.shape, k.shape
     cfg.out_stride = _rows(who, "out", out, dt, qs, dev)
     cfg.dout_stride = _rows(who, "dout", dout, dt, qs, dev)
     _same(who, "lse", lse, torch.float32, (cfg.n_q_heads, cfg.rows), dev)
+    new = torch.empty if cfg.n_seqs > 0 else torch.zeros
     if dq is None:
-        dq = torch.empty(qs, dtype=dt, device=dev)
+        dq = new(qs, dtype=dt, device=dev)
+        cfg.clear |= L.CLEAR_DQ
     else:
         cfg.dq_stride = _rows(who, "dq", dq, dt, qs, dev)
     if dk is None:
-        dk = torch.empty(ks, dtype=dt, device=dev)
+        dk = new(ks, dtype=dt, device=dev)
+        cfg.clear |= L.CLEAR_DK
     else:
         cfg.dk_stride = _rows(who, "dk", dk, dt, ks, dev)
     if dv is None:
-        dv = torch.empty(ks, dtype=dt, device=dev)
+        dv = new(ks, dtype=dt, device=dev)
+        cfg.clear |= L.CLEAR_DV
     else:
         cfg.dv_stride = _rows(who, "dv", dv, dt, ks, dev)
     need = _need(_lib.tandem_attention_workspace_size, cfg)

@@ -212,3 +212,10 @@ def test_refuses_more_than_a_launch_covers():
         assert _status(L.lib.tandem_attention, C.byref(c), P, P, P, P, P, P, None) == L.E_SHAPE
         assert _status(L.lib.tandem_attention_backward, C.byref(c), P, P, P, P, P, P, P, P, P, P, WS, 1 << 20,
                        None) == L.E_SHAPE
+
+
+@pytest.mark.parametrize("clear", [-1, 32, 1 << 20])
+def test_attention_refuses_outputs_to_clear_that_there_are_not(clear):
+    c = _attn(clear=clear)
+    assert _status(L.lib.tandem_attention, C.byref(c), P, P, P, P, P, P, None) == L.E_ARG
+    assert _status(L.lib.tandem_attention_backward, C.byref(c), P, P, P, P, P, P, P, P, P, P, WS, 1 << 20, None) == L.E_ARG
