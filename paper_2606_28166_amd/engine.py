@@ -266,6 +266,14 @@ def _run(dev, fn, *args) -> None:
         L.check(status)
 
 
+def _written(*tensors: Optional[torch.Tensor]) -> None:
+    """Tells autograd that these tensors of the caller's (None: not given) hold other values
+    now: a graph that saved one of them refuses its backward pass instead of using the new values."""
+    for t in tensors:
+        if t is not None:
+            torch._C._increment_version([t])
+
+
 def _need(fn, *args) -> int:
     """The workspace that a *_workspace_size call asks for."""
     n = C.c_size_t()
@@ -350,12 +358,14 @@ def token_logprob_backward(logits: torch.Tensor, tokens: torch.Tensor, fwd, g_lo
         _same(who, "fwd['lse_diff']", diff, torch.float32, row, dev)
     else:
         ref = None
+    given = out
     if out is None:
         out = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
     else:
         cfg.grad_stride = _rows(who, "out", out, logits.dtype, logits.shape, dev)
     _run(dev, _lib.tandem_token_logprob_backward, cfg, logits.data_ptr(), _ptr(ref), tokens.data_ptr(),
          lse.data_ptr(), _ptr(kl), _ptr(diff), g_logp.data_ptr(), _ptr(g_kl), out.data_ptr())
+    _written(given)
     return out
 
 
@@ -410,6 +420,7 @@ def qk_norm_rope_backward(qkv: torch.Tensor, positions: torch.Tensor, dq: torch.
     N, hd, dt = cfg.rows, cfg.head_dim, qkv.dtype
     cfg.q_stride = _rows(who, "dq", dq, dt, (N, n_q, hd), dev)
     cfg.k_stride = _rows(who, "dk", dk, dt, (N, n_kv, hd), dev)
+    given = dqkv
     if dqkv is None:
         dqkv = torch.empty_strided(qkv.shape, (cfg.qkv_stride, 1), dtype=dt, device=dev)
         dqkv[:, (n_q + n_kv) * hd:].zero_()
@@ -418,6 +429,7 @@ def qk_norm_rope_backward(qkv: torch.Tensor, positions: torch.Tensor, dq: torch.
     if q_gain is None:
         _run(dev, _lib.tandem_qk_norm_rope_backward, cfg, qkv.data_ptr(), None, None, positions.data_ptr(),
              dq.data_ptr(), dk.data_ptr(), dqkv.data_ptr(), None, None, None, 0)
+        _written(given)
         return dict(dqkv=dqkv, dq_gain=None, dk_gain=None)
     gain = torch.empty((2, hd), dtype=torch.float32, device=dev)
     p = gain.data_ptr()
@@ -425,6 +437,7 @@ def qk_norm_rope_backward(qkv: torch.Tensor, positions: torch.Tensor, dq: torch.
     workspace = _workspace(workspace, need, dev)
     _run(dev, _lib.tandem_qk_norm_rope_backward, cfg, qkv.data_ptr(), q_gain.data_ptr(), k_gain.data_ptr(),
          positions.data_ptr(), dq.data_ptr(), dk.data_ptr(), dqkv.data_ptr(), p, p + 4 * hd, workspace.data_ptr(), need)
+    _written(given)
     dgq, dgk = gain.unbind(0)
     return dict(dqkv=dqkv, dq_gain=dgq, dk_gain=dgk)
 
@@ -459,6 +472,7 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets: torch.
     cfg, dt, dev = _attention_cfg("attention", q, k, v, offsets, scale)
     new = torch.empty if cfg.n_seqs > 0 else torch.zeros          # the library clears beside sequences only
     cfg.clear = L.CLEAR_LSE
+    given = out
     if out is None:
         out = new(q.shape, dtype=dt, device=dev)
         cfg.clear |= L.CLEAR_OUT
@@ -467,6 +481,7 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets: torch.
     lse = new((cfg.n_q_heads, cfg.rows), dtype=torch.float32, device=dev)
     _run(dev, _lib.tandem_attention, cfg, q.data_ptr(), k.data_ptr(), v.data_ptr(), offsets.data_ptr(), out.data_ptr(),
          lse.data_ptr())
+    _written(given)
     return dict(out=out, lse=lse)
 
 
@@ -486,6 +501,7 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
     cfg.dout_stride = _rows(who, "dout", dout, dt, qs, dev)
     _same(who, "lse", lse, torch.float32, (cfg.n_q_heads, cfg.rows), dev)
     new = torch.empty if cfg.n_seqs > 0 else torch.zeros
+    given = (dq, dk, dv)
     if dq is None:
         dq = new(qs, dtype=dt, device=dev)
         cfg.clear |= L.CLEAR_DQ
@@ -506,6 +522,7 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
     _run(dev, _lib.tandem_attention_backward, cfg, dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(),
          out.data_ptr(), lse.data_ptr(), offsets.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
          _ptr(workspace), need)
+    _written(*given)
     return dict(dq=dq, dk=dk, dv=dv)
 
 
@@ -516,7 +533,8 @@ class AdamW:
     learning rates of 1e-6 it would otherwise not move).
 
     params: contiguous bfloat16 or float32 tensors on one GPU that share no
-    memory, updated in place.
+    memory, updated in place (as autograd knows: a graph that saved a weight before a
+    step does not run backward after it).
     weight_decay: one number, or one per tensor.  max_norm > 0 clips by the
     global norm of the gradients.  master None: where any weight is bfloat16.
     state: what state() returned, to resume (its tensors are used, not copied)."""
@@ -622,5 +640,6 @@ class AdamW:
         workspace = _workspace(None, need, self.dev)
         _run(self.dev, _lib.tandem_adamw, cfg, self._table, len(types), self.m.data_ptr(), self.v.data_ptr(),
              _ptr(self.master), _ptr(norm), _ptr(workspace), need)
+        torch._C._increment_version(self.params)       # for graphs that saved a weight
         self.steps += 1
         return norm
