@@ -753,7 +753,8 @@ __device__ __forceinline__ void store_column(float* p, const f32x16_t* acc, floa
              acc[d][4 * j + 3] * by);
 }
 
-// One of the even parts of a list, of 2^25 steps and 16 parts at most.
+// One of the even parts of a list, of 2^26 steps (a launch over the queries has fewer than 2^24
+// workgroups of 128 rows of a head) and 16 parts at most.
 struct Share {
   int begin, count;
 };
@@ -1058,7 +1059,7 @@ __global__ __launch_bounds__(256) void flash_join_kernel(FlashArgs a, int width,
   store4(out + c + 4, hi[0], hi[1], hi[2], hi[3]);
 }
 
-int slots_of(const FlashArgs& a, int per) { return a.N / per + a.n_seqs; }
+int64_t slots_of(const FlashArgs& a, int per) { return (int64_t)a.N / per + a.n_seqs; }
 
 // Whether the tiles of queries are so few that the keys are shared out: below two workgroups per
 // compute unit, if there are tiles enough to share (with one tile of a wave in LDS, more).
@@ -1073,40 +1074,62 @@ bool few_queries(const FlashArgs& a) {
   return workgroups < 512 && a.N / a.n_seqs >= (Alone<T, HD>::TURNS == 2 ? 160 : 512);
 }
 
+// Workgroups, each of 256 threads, of the passes over the queries (forward, dQ) and over the keys, and
+// of the parts' sums.
+template <typename T, int HD>
+int64_t query_blocks(const FlashArgs& a) {
+  if (few_queries<T, HD>(a)) return slots_of(a, 32) * a.nq;
+  const int together = heads_together(a.nq / a.nkv);
+  return slots_of(a, 32 * (kWaves / together)) * (a.nq / together);
+}
+template <typename T, int HD>
+int parts_of(const FlashArgs& a) {
+  return flash_parts(a.N, a.n_seqs, a.nq, a.nkv, HD, sizeof(T) == 2 ? DT_BF16 : DT_F32);
+}
+template <typename T, int HD>
+int64_t key_blocks(const FlashArgs& a, int parts) {
+  return slots_of(a, 32 * (kByPairs<T, HD> ? kPairs : kWaves)) * a.nkv * parts;
+}
+template <int HD>
+int64_t join_blocks(const FlashArgs& a) { return ((int64_t)a.N * a.nkv * HD / 8 + 255) / 256; }
+
+template <typename T, int HD>
+int64_t most_blocks(const FlashArgs& a, bool backward) {
+  const int64_t queries = query_blocks<T, HD>(a);
+  if (!backward) return queries;
+  const int parts = parts_of<T, HD>(a);
+  return std::max({queries, key_blocks<T, HD>(a, parts), parts > 1 ? 2 * join_blocks<HD>(a) : 0});
+}
+
 template <typename T, int HD>
 hipError_t run(const FlashArgs& a, hipStream_t st) {
-  if (few_queries<T, HD>(a)) {
-    flash_alone_kernel<T, HD><<<(unsigned)(slots_of(a, 32) * (int64_t)a.nq), 64 * kWaves, 0, st>>>(a);
-    return hipGetLastError();
-  }
-  const int group = a.nq / a.nkv, together = heads_together(group);
-  const int slots = slots_of(a, 32 * (kWaves / together));
-  flash_kernel<T, HD><<<(unsigned)(slots * (int64_t)a.nkv * (group / together)), 64 * kWaves, 0, st>>>(a);
+  const unsigned grid = (unsigned)query_blocks<T, HD>(a);
+  if (few_queries<T, HD>(a))
+    flash_alone_kernel<T, HD><<<grid, 64 * kWaves, 0, st>>>(a);
+  else
+    flash_kernel<T, HD><<<grid, 64 * kWaves, 0, st>>>(a);
   return hipGetLastError();
 }
 
 template <typename T, int HD>
 hipError_t run_backward(const FlashArgs& a, hipStream_t st) {
-  const int group = a.nq / a.nkv, together = heads_together(group);
-  if (few_queries<T, HD>(a)) {
-    flash_dq_alone_kernel<T, HD><<<(unsigned)(slots_of(a, 32) * (int64_t)a.nq), 64 * kWaves, 0, st>>>(a);
-  } else {
-    const int slots = slots_of(a, 32 * (kWaves / together));
-    flash_dq_kernel<T, HD><<<(unsigned)(slots * (int64_t)a.nkv * (group / together)), 64 * kWaves, 0, st>>>(a);
-  }
+  const unsigned queries = (unsigned)query_blocks<T, HD>(a);
+  if (few_queries<T, HD>(a))
+    flash_dq_alone_kernel<T, HD><<<queries, 64 * kWaves, 0, st>>>(a);
+  else
+    flash_dq_kernel<T, HD><<<queries, 64 * kWaves, 0, st>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int parts = flash_parts(a.N, a.n_seqs, a.nq, a.nkv, HD, sizeof(T) == 2 ? DT_BF16 : DT_F32);
-  const int64_t along = (int64_t)a.nkv * parts;
+  const int parts = parts_of<T, HD>(a);
+  const unsigned keys = (unsigned)key_blocks<T, HD>(a, parts);
   if constexpr (kByPairs<T, HD>)
-    flash_dkv_pair_kernel<HD><<<(unsigned)(slots_of(a, 32 * kPairs) * along), 128 * kPairs, 0, st>>>(a, parts);
+    flash_dkv_pair_kernel<HD><<<keys, 128 * kPairs, 0, st>>>(a, parts);
   else
-    flash_dkv_kernel<T, HD><<<(unsigned)(slots_of(a, 32 * kWaves) * along), 64 * kWaves, 0, st>>>(a, parts);
+    flash_dkv_kernel<T, HD><<<keys, 64 * kWaves, 0, st>>>(a, parts);
   if (parts > 1) {
     const hipError_t f = hipGetLastError();
     if (f != hipSuccess) return f;
-    const int width = a.nkv * HD;
-    flash_join_kernel<T><<<dim3((unsigned)(((int64_t)a.N * width / 8 + 255) / 256), 2), 256, 0, st>>>(a, width, parts);
+    flash_join_kernel<T><<<dim3((unsigned)join_blocks<HD>(a), 2), 256, 0, st>>>(a, a.nkv * HD, parts);
   }
   return hipGetLastError();
 }
@@ -1136,11 +1159,12 @@ int flash_parts(int N, int n_seqs, int nq, int nkv, int hd, int dtype) {
   return most < 2 ? 1 : (int)std::min(most, std::max<int64_t>(4, (want + tiles) / (tiles + 1)));
 }
 
-int64_t flash_blocks(int N, int n_seqs, int nq, int nkv) {
-  // per = 128 / together positions to a slot and nq / together workgroups; of pairs, 64 positions
-  // and nkv * parts <= nq
-  const int64_t forward = ((int64_t)N / 128 + n_seqs + 1) * nq, pairs = ((int64_t)N / 64 + n_seqs) * nq;
-  return forward > pairs ? forward : pairs;
+int64_t flash_blocks(const FlashArgs& a, int hd, int dtype, bool backward) {
+  if (a.N < 1 || a.n_seqs < 1) return 0;
+  const bool b16 = dtype == DT_BF16;
+  if (hd == 32) return b16 ? most_blocks<bf16_t, 32>(a, backward) : most_blocks<float, 32>(a, backward);
+  if (hd == 64) return b16 ? most_blocks<bf16_t, 64>(a, backward) : most_blocks<float, 64>(a, backward);
+  return b16 ? most_blocks<bf16_t, 128>(a, backward) : most_blocks<float, 128>(a, backward);
 }
 
 #define TANDEM_FLASH_DISPATCH(fn)                                                            \

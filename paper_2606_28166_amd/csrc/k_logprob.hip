@@ -590,7 +590,9 @@ int logprob_splits(int R, int V, int* chunk) {
 }
 
 int64_t logprob_blocks(int R, int V) {
-  const int64_t forward = V <= 2048 ? ((int64_t)R + 3) / 4 : R;
+  int chunk = 0;
+  const int splits = logprob_splits(R, V, &chunk);
+  const int64_t forward = splits > 1 ? (int64_t)R * splits : V <= 2048 ? ((int64_t)R + 3) / 4 : R;
   const int64_t backward = (int64_t)R * ((V + kGradChunk - 1) / kGradChunk);
   return forward > backward ? forward : backward;
 }

@@ -164,10 +164,10 @@ tandem_status attention_check(const char* who, const tandem_attention_cfg* c, bo
       {"dk_stride", c->dk_stride, kv},    {"dv_stride", c->dv_stride, kv}};
   for (int i = 0; i < (backward ? 8 : 4); ++i)
     if ((s = stride_check(who, st[i].what, st[i].stride, st[i].least, c->dtype)) != TANDEM_OK) return s;
-  if (flash_blocks(c->rows, c->n_seqs, c->n_q_heads, c->n_kv_heads) > kMaxGrid)
-    return refuse(TANDEM_E_SHAPE, "%s: rows and sequences times heads exceed what one launch covers", who);
   *a = FlashArgs{};
   a->N = c->rows; a->n_seqs = c->n_seqs; a->nq = c->n_q_heads; a->nkv = c->n_kv_heads;
+  if (flash_blocks(*a, c->head_dim, c->dtype, backward) > kMaxGrid)
+    return refuse(TANDEM_E_SHAPE, "%s: rows and sequences times heads exceed what one launch covers", who);
   a->scale = c->scale;
   a->ldq = c->q_stride; a->ldk = c->k_stride; a->ldv = c->v_stride; a->ldo = c->out_stride;
   a->lddo = c->dout_stride; a->lddq = c->dq_stride; a->lddk = c->dk_stride; a->lddv = c->dv_stride;

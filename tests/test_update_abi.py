@@ -219,3 +219,16 @@ def test_attention_refuses_outputs_to_clear_that_there_are_not(clear):
     c = _attn(clear=clear)
     assert _status(L.lib.tandem_attention, C.byref(c), P, P, P, P, P, P, None) == L.E_ARG
     assert _status(L.lib.tandem_attention_backward, C.byref(c), P, P, P, P, P, P, P, P, P, P, WS, 1 << 20, None) == L.E_ARG
+
+
+def test_attention_takes_what_its_launches_cover():
+    """The limit is that of the launches a call makes: 2^25 rows of 32 heads of 32 on 8 are 2^23 workgroups
+    over the queries and 2^21 over the keys, whatever other shapes would take."""
+    wide = dict(n_q_heads=32, n_kv_heads=8, head_dim=32, q_stride=1024, k_stride=256, v_stride=256, out_stride=1024,
+                dout_stride=1024, dq_stride=1024, dk_stride=256, dv_stride=256)
+    for rows in (1 << 25, (1 << 26) - 128):
+        assert L.tandem_attention_workspace_size(_attn(rows=rows, **wide)) >= 2 * rows * 32 * 4
+    c = _attn(rows=1 << 26, **wide)                               # 2^24 workgroups and two more for the sequences
+    assert _status(L.lib.tandem_attention_workspace_size, C.byref(c), C.byref(C.c_size_t())) == L.E_SHAPE
+    assert _status(L.lib.tandem_attention, C.byref(c), P, P, P, P, P, P, None) == L.E_SHAPE
+    assert L.tandem_attention_workspace_size(_attn(n_seqs=0)) >= 0 and L.tandem_attention_workspace_size(_attn(rows=0)) >= 0
