@@ -25,6 +25,7 @@
 
 #include "common.h"
 #include "update.h"
+#include "update_plan.h"
 
 namespace tandem {
 namespace {
@@ -33,7 +34,7 @@ typedef short s16x4_v __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4_v lds_s16x4_v;
 
 constexpr int kRows = 64;        // rows of a staged tile
-constexpr int kWaves = 4;        // waves of a workgroup
+constexpr int kWaves = kFlashWaves;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -367,14 +368,6 @@ __device__ __forceinline__ void clear_dkv(const FlashArgs& a) {
   if (a.clear & TANDEM_CLEAR_DV) clear_rows<T>(a, a.dv, a.lddv, a.nkv * HD);
 }
 
-// Query heads of a key head that share a workgroup (the rest of its waves take other
-// positions): the largest power of two that divides the group, up to the waves.
-__host__ __device__ inline int heads_together(int group) {
-  int n = 1;
-  while (2 * n <= kWaves && group % (2 * n) == 0) n *= 2;
-  return n;
-}
-
 // The other half wave's value (lane l and l + 32 hold the same column).
 __device__ __forceinline__ float other_max(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -490,9 +483,7 @@ template <typename T, int HD>
 struct Alone {
   using O = Ops<T, HD>;
   static constexpr int TILE = 32 * O::ROW;
-  // 64 KB at most for four waves' tiles of keys and values, so two workgroups to a compute unit: one
-  // sequence of 4000, 8 heads of 128 on 1, 53 us; two in turn and one workgroup 81
-  static constexpr int TURNS = TILE <= 4096 ? 2 : 1;
+  static constexpr int TURNS = two_turns(HD, sizeof(T) == 2) ? 2 : 1;
   static constexpr int PART = 32 * HD * 4;                 // bytes of a wave's accumulator
   typedef char Room[kWaves][TURNS][2][TILE];
   static_assert(sizeof(Room) >= kWaves * PART && PART >= TILE, "room for the accumulators and the results");
@@ -637,7 +628,7 @@ __device__ __forceinline__ void dq_tile(f32x16_t* dq, const char* __restrict__ t
 // rounding P itself to bf16 would round dS twice).  The results are scaled back exactly.
 constexpr float kProbScale = 32768.f, kProbBits = 15.f;
 template <typename T, int HD>
-constexpr bool kByPairs = sizeof(T) == 2 && HD >= 64;     // dK and dV by pairs of waves
+constexpr bool kByPairs = keys_by_pairs(HD, sizeof(T) == 2);
 
 // What a lane holds of its query, and leaves for the pass over the keys (if `leave`): the delta
 // dout . out (negated) and the log-sum-exp in powers of two.
@@ -1061,30 +1052,20 @@ __global__ __launch_bounds__(256) void flash_join_kernel(FlashArgs a, int width,
 
 int64_t slots_of(const FlashArgs& a, int per) { return (int64_t)a.N / per + a.n_seqs; }
 
-// Whether the tiles of queries are so few that the keys are shared out: below two workgroups per
-// compute unit, if there are tiles enough to share (with one tile of a wave in LDS, more).
-// Forward, us: one sequence of 2000, float32, 4 heads of 32 on 2, 79 and shared 27; bf16, one of 8703, 2 heads
-// of 64 on 2, 131 and 46; one of 2000, 16 of 128 on 8, 45 and 36.  Not so few: 64 of at most 1000,
-// float32, 98 and 122; one of 8703, 16 of 64 on 4, 187 and 287.  Short: eight of at most 373, 16 of
-// 128 on 8, 16 and 19; 20 of at most 299, 8 of 64 on 2, backward 36 and 40.
 template <typename T, int HD>
-bool few_queries(const FlashArgs& a) {
-  const int together = heads_together(a.nq / a.nkv);
-  const int64_t workgroups = ((int64_t)a.N * together / (32 * kWaves) + a.n_seqs / 2) * (a.nq / together);
-  return workgroups < 512 && a.N / a.n_seqs >= (Alone<T, HD>::TURNS == 2 ? 160 : 512);
-}
+bool shared_keys(const FlashArgs& a) { return few_queries(a.N, a.n_seqs, a.nq, a.nkv, HD, sizeof(T) == 2); }
 
 // Workgroups, each of 256 threads, of the passes over the queries (forward, dQ) and over the keys, and
 // of the parts' sums.
 template <typename T, int HD>
 int64_t query_blocks(const FlashArgs& a) {
-  if (few_queries<T, HD>(a)) return slots_of(a, 32) * a.nq;
+  if (shared_keys<T, HD>(a)) return slots_of(a, 32) * a.nq;
   const int together = heads_together(a.nq / a.nkv);
   return slots_of(a, 32 * (kWaves / together)) * (a.nq / together);
 }
 template <typename T, int HD>
 int parts_of(const FlashArgs& a) {
-  return flash_parts(a.N, a.n_seqs, a.nq, a.nkv, HD, sizeof(T) == 2 ? DT_BF16 : DT_F32);
+  return flash_parts(a.N, a.n_seqs, a.nq, a.nkv, HD, sizeof(T) == 2);
 }
 template <typename T, int HD>
 int64_t key_blocks(const FlashArgs& a, int parts) {
@@ -1104,7 +1085,7 @@ int64_t most_blocks(const FlashArgs& a, bool backward) {
 template <typename T, int HD>
 hipError_t run(const FlashArgs& a, hipStream_t st) {
   const unsigned grid = (unsigned)query_blocks<T, HD>(a);
-  if (few_queries<T, HD>(a))
+  if (shared_keys<T, HD>(a))
     flash_alone_kernel<T, HD><<<grid, 64 * kWaves, 0, st>>>(a);
   else
     flash_kernel<T, HD><<<grid, 64 * kWaves, 0, st>>>(a);
@@ -1114,7 +1095,7 @@ hipError_t run(const FlashArgs& a, hipStream_t st) {
 template <typename T, int HD>
 hipError_t run_backward(const FlashArgs& a, hipStream_t st) {
   const unsigned queries = (unsigned)query_blocks<T, HD>(a);
-  if (few_queries<T, HD>(a))
+  if (shared_keys<T, HD>(a))
     flash_dq_alone_kernel<T, HD><<<queries, 64 * kWaves, 0, st>>>(a);
   else
     flash_dq_kernel<T, HD><<<queries, 64 * kWaves, 0, st>>>(a);
@@ -1135,29 +1116,6 @@ hipError_t run_backward(const FlashArgs& a, hipStream_t st) {
 }
 
 }  // namespace
-
-int flash_parts(int N, int n_seqs, int nq, int nkv, int hd, int dtype) {
-  if (n_seqs < 1) return 1;
-  // Tiles of keys (64, or 128 of the other form) differ in work by as much as their sequence is
-  // long.  Below a workgroup per compute unit, and the longer the sequences below the more rounds
-  // of those that fit the device together, they are cut into parts that give `want`
-  // workgroups, four at least, unless a part would be shorter than about 8 steps.  Backward pass whole and
-  // in parts, us:
-  //   bf16    one sequence of 32768, 16 heads of 64 on 4, 8256 and 7635; four of 4096 720 and 571;
-  //           three of 2048, 32 of 128 on 8, 489 and 434; 20 of at most 1973, 8 of 64 on 2, 223 and 186
-  //   float32 four of at most 7998, 4 heads of 32 on 2, 1598 and 758; one of 2000, 16 heads of 64
-  //           on 4, 1243 and 386
-  // Of short ones the sums cost more than the evenness gains: bf16, 24 of 1200, heads of 64, 362
-  // and 406; six of 1100, heads of 128, 276 and 308; eight of at most 253, 16 heads of 128 on 8, 33
-  // and 49.
-  const bool pairs = dtype == DT_BF16 && hd >= 64;
-  const int64_t tiles = (N / (pairs ? 64 : 128) + n_seqs / 2) * (int64_t)nkv, len = N / n_seqs;
-  const int64_t want = pairs && hd == 128 ? 1024 : 2048;
-  const int64_t few = std::min(want, want * len / (pairs ? 2048 : 512));
-  if (tiles > std::max<int64_t>(256, few)) return 1;
-  const int64_t most = std::min<int64_t>(16, len * (nq / nkv) / (pairs ? 256 : 64));
-  return most < 2 ? 1 : (int)std::min(most, std::max<int64_t>(4, (want + tiles) / (tiles + 1)));
-}
 
 int64_t flash_blocks(const FlashArgs& a, int hd, int dtype, bool backward) {
   if (a.N < 1 || a.n_seqs < 1) return 0;

@@ -9,6 +9,7 @@
 #include "status.h"
 #include "tandem.h"
 #include "update.h"
+#include "update_plan.h"
 
 using namespace tandem;
 
@@ -178,7 +179,7 @@ tandem_status attention_check(const char* who, const tandem_attention_cfg* c, bo
 // The backward pass's workspace: two statistics per row and head, and the sums of the parts.
 size_t attention_stat_bytes(const FlashArgs& a) { return up256((size_t)a.N * a.nq * sizeof(float)); }
 size_t attention_bytes(const FlashArgs& a, int hd, int dtype) {
-  const int parts = flash_parts(a.N, a.n_seqs, a.nq, a.nkv, hd, dtype);
+  const int parts = flash_parts(a.N, a.n_seqs, a.nq, a.nkv, hd, dtype == TANDEM_BF16);
   return 2 * attention_stat_bytes(a) + (parts > 1 ? (size_t)2 * parts * a.N * a.nkv * hd * sizeof(float) : 0);
 }
 

@@ -63,7 +63,6 @@ struct FlashArgs {
   int clear;                               // TANDEM_CLEAR_*
   float* sums;                             // and [dV, dK][parts][N][nkv][hd], where the work on a tile is cut into parts
 };
-int flash_parts(int N, int n_seqs, int nq, int nkv, int hd, int dtype);
 // workgroups of the largest launch (a.N, n_seqs, nq, nkv)
 int64_t flash_blocks(const FlashArgs& a, int hd, int dtype, bool backward);
 hipError_t launch_flash(const FlashArgs& a, int hd, int dtype, hipStream_t st);
