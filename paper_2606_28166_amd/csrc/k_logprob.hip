@@ -531,9 +531,10 @@ __global__ __launch_bounds__(256) void logprob_grad_kernel(LogprobArgs a, int pa
   const float at = g * a.inv_t, lse = a.lse[r];
   const bool near = fabsf(lse) < kGradMost<T>;             // false of a NaN
   if (REF && k != 0.f) {
-    const float mean = a.diff[r] + a.kl[r];
-    if (near && fabsf(mean) < kGradMost<T>) {
-      const RowGrad q = {a.inv_t * (-g - k * mean), a.inv_t * k * a.inv_t, at, lse, a.inv_t};
+    const float mean = a.diff[r] + a.kl[r], B = a.inv_t * k * a.inv_t;
+    // B of a temperature below 1e-19 may be infinite, and what it is times 0
+    if (near && fabsf(mean) < kGradMost<T> && fabsf(B) < INFINITY) {
+      const RowGrad q = {a.inv_t * (-g - k * mean), B, at, lse, a.inv_t};
       grad_chunk<T, true>(a, q, z, zr, out, y, v0, v1);
     } else if (part == 0) {
       logit_grad<T, true>(a, g, k, z, zr, out, y);

@@ -171,3 +171,20 @@ def test_logprob_gradient_of_large_rows(R, V, dt):
         _gradient_check(b, z, None, tok, gl, None, T64, dt)
         assert torch.equal(z, keep)
         assert torch.equal(E.token_logprob_backward(z, tok, f, gl, g_kl=gk, ref=zr, temperature=T, out=z), a)
+
+
+@pytest.mark.parametrize("dt", [BF, F32], ids=["bf16", "f32"])
+def test_logprob_gradient_at_the_smallest_temperatures(dt):
+    """1 / T^2 passes float32: models that agree everywhere have a KL of 0 and no gradient of it."""
+    from paper_2606_28166_amd import engine as E
+    for T in (1e-19, 1e-25, 4e-39):
+        for V in (50, 9000):
+            z, _, tok, gl, gk = _inputs(3, V, dt, 0.0, 0.0, V)
+            z.fill_(0.0)
+            gl.mul_(0.25)                                    # g / T stays in the type
+            f = E.token_logprob(z, tok, ref=z.clone(), temperature=T)
+            assert (f["kl"] == 0).all() and (f["lse_diff"] == 0).all()
+            g = E.token_logprob_backward(z, tok, f, gl, g_kl=gk, ref=z.clone(), temperature=T)
+            hot = torch.zeros((3, V), dtype=F64, device=z.device).scatter_(1, tok.long()[:, None], 1.0)
+            want = gl.to(F64)[:, None] * (hot - 1.0 / V) * float(1.0 / torch.tensor(T, dtype=F32))
+            _within(g, want, (_half(dt) + 64 * U) * want.abs(), "grad")
