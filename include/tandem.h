@@ -419,7 +419,10 @@ tandem_status tandem_qk_norm_rope_backward(const tandem_qk_cfg* cfg, const void*
  * bf16 for the products that take them.
  * The inputs must be finite: a NaN or infinity in a row of v, in the backward
  * pass of any input, may reach other rows of the same sequence, never another
- * sequence.
+ * sequence.  Scores must stay below 2^20 in magnitude.  They are float32 sums, and the
+ * backward pass takes probabilities from the float32 lse: relative errors of up to
+ * (head_dim + 8) 2^-24 scale sum |q||k| and 2^-21 |lse|, so at that size no digit
+ * is left, and beyond it results may be infinite or NaN.
  * Heads of a row are contiguous ([n][head_dim]); arrays are 16-byte aligned
  * and strides multiples of 16 bytes, so q, k and v may be columns of one
  * projection. */

@@ -11,7 +11,7 @@ import math
 import pytest
 import torch
 
-from tests.test_gpu_update import BF, DEV, F32, F64, LENS, U, _attention_inputs, _half, _say, _within
+from tests.test_gpu_update import BF, DEV, F32, F64, LENS, U, _attention_inputs, _gen, _half, _say, _within
 from tests.update_forms import FORMS
 
 pytestmark = pytest.mark.gpu
@@ -114,3 +114,43 @@ def test_attention_clamps_offsets(offs, dt):
         assert (f[name][~live] == 7.0).all(), name
         _within(f[name][live], ref[name][live], tol[name][live], name)
     _within(f["lse"], ref["lse"], tol["lse"], "lse")
+
+
+@pytest.mark.parametrize("dt", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("nq,nkv,hd", [(2, 1, 32), (4, 1, 64), (2, 2, 128)])
+def test_attention_of_large_scores(nq, nkv, hd, dt):
+    """Scores of 2^19 and -2^19, exact in float32: the keys of the higher score share a query's probability.  Forward
+    they are exact; backward a probability comes from the float32 log-sum-exp, whose exponent is off by 7 roundings
+    of 2^19 log2 e at most: 0.32, a factor of 1.25."""
+    from paper_2606_28166_amd import engine as E
+    n = 150
+    g = _gen(hd)
+    x = 2.0 ** 19 / (hd * 0.125)                              # scale hd q k = 2^19 with scale 1 / 8
+    side = (torch.rand((n,), generator=g, device=DEV) < 0.5).float() * 2 - 1
+    side[0] = 1
+    q = torch.full((n, nq, hd), 1.0, device=DEV).to(dt)
+    k = (side * x)[:, None, None].expand(n, nkv, hd).to(dt).contiguous()
+    v = torch.randn((n, nkv, hd), generator=g, device=DEV).to(dt)
+    dout = torch.randn((n, nq, hd), generator=g, device=DEV).to(dt)
+    o = torch.tensor([0, n], dtype=torch.int32, device=DEV)
+    f = E.attention(q, k, v, o, scale=0.125)
+    p = ((side > 0)[None] & torch.ones((n, n), dtype=torch.bool, device=DEV).tril()).to(F64)
+    p = p / p.sum(1, keepdim=True)
+    for h in range(nq):
+        V = v[:, h * nkv // nq].to(F64)
+        out = p @ V
+        _within(f["out"][:, h], out, (2 * _half(dt) + 200 * U) * (p @ V.abs()), "out")
+        want = 2.0 ** 19 + (p > 0).sum(1).to(F64).log()
+        _within(f["lse"][h], want, 3 * U * want, "lse")
+    b = E.attention_backward(dout, q, k, v, f["out"], f["lse"], o, scale=0.125)
+    bound = {name: torch.zeros(t.shape, dtype=F64, device=DEV) for name, t in (("dq", q), ("dk", k), ("dv", v))}
+    for h in range(nq):
+        j = h * nkv // nq
+        D, V = dout[:, h].to(F64), v[:, j].to(F64)
+        dp = D @ V.t().contiguous()
+        off = 1.3 * p * (dp.abs() + (D * (p @ V)).sum(1, keepdim=True).abs() + 0.1 * (D.abs() * (p @ V.abs())).sum(1, keepdim=True))
+        bound["dq"][:, h] = off @ k[:, j].to(F64).abs() * 0.125
+        bound["dk"][:, j] += off.t().contiguous() @ q[:, h].to(F64).abs() * 0.125
+        bound["dv"][:, j] += 1.3 * p.t().contiguous() @ D.abs()
+    for name in bound:
+        _within(b[name], torch.zeros_like(bound[name]), bound[name] + 1e-30, name)      # finite, and of the terms' size
