@@ -7,8 +7,8 @@
 // squares per chunk in 64 bits (a gradient of 1e20 or 1e-25 squares without
 // overflow or loss), a second adds them up in a fixed order, and the update reads
 // the factor from memory: no host synchronisation and no atomics.  Two layers of a
-// d_model 2560 / FFN 9728 model (202 million weights): 1.06 ms for the update, 5.4 TB/s, and 0.12 for
-// the sums of squares, 3.4 TB/s, also with a chunk's loads all ahead.
+// d_model 2560 / FFN 9728 model (202 million weights): 0.92 to 1.06 ms from card to card for the update, 5.4
+// to 6.2 TB/s, and 0.10 to 0.12 for the sums of squares, 3.4 to 3.9 TB/s, also with a chunk's loads all ahead.
 #include "common.h"
 #include "update.h"
 

@@ -20,7 +20,8 @@
 // In bf16 models the probabilities and score gradients are rounded to bf16 where the next
 // product takes them (float32 operands run at a sixteenth of the rate), and dout . out takes the
 // output as it was rounded: 1.7e-3 and 1.0e-3 of the norm of dQ and dK, beside the 1.7e-3 of
-// their own rounding.  Scores, sums, maxima and accumulators are float32.
+// their own rounding; 1.5e-3 of the output's norm for its probabilities, beside 1.6e-3.
+// Scores, sums, maxima and accumulators are float32.
 #include <algorithm>
 
 #include "common.h"
@@ -237,17 +238,15 @@ __device__ __forceinline__ void load_floats(float* dst, const float* g, int vali
   __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t*)dst, 4, lane * 4, 0, 0, 0);
 }
 
-// All but the LEFT newest loads of this wave have arrived, its LDS reads and writes are done;
-// then the workgroup's waves meet.
-template <int LEFT = 0>
+// This wave's loads have arrived, its LDS reads and writes are done.
+__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+
+// The same of every wave of the workgroup.
 __device__ __forceinline__ void meet() {
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LEFT) : "memory");
+  arrived();
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
-
-// The same of this wave alone.
-__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
 
 __device__ __forceinline__ void store4(bf16_t* p, float a, float b, float c, float d) {
   typedef __bf16 bf16x4_v __attribute__((ext_vector_type(4)));
@@ -418,7 +417,7 @@ struct Softmax {
 // Bound by latency more than by any one pipe (the matrix pipe is busy 56% of the cycles): what
 // counts is the waves a SIMD holds, so the tiles are of 32 keys and the code keeps nothing
 // ahead.  Heads of 128 take 161 registers, three waves a SIMD: sixteen ragged rollouts (32 heads
-// on 8) 278 us, 0.9 PFLOP/s.  Two waves with
+// on 8) 275 us, 0.9 PFLOP/s.  Two waves with
 // tiles of 64 and the scores, exponentials and value products of three blocks
 // interleaved in each took 314, two without that 325.
 template <typename T, int HD>
@@ -485,6 +484,7 @@ struct Alone {
   static constexpr int TILE = 32 * O::ROW;
   static constexpr int TURNS = two_turns(HD, sizeof(T) == 2) ? 2 : 1;
   static constexpr int PART = 32 * HD * 4;                 // bytes of a wave's accumulator
+  static constexpr int WGS = TURNS * TILE <= 8192 ? 2 : 1; // workgroups per compute unit (LDS: 64 KB, or 128)
   typedef char Room[kWaves][TURNS][2][TILE];
   static_assert(sizeof(Room) >= kWaves * PART && PART >= TILE, "room for the accumulators and the results");
   struct Work {                                            // of this workgroup
@@ -552,7 +552,7 @@ struct Alone {
 };
 
 template <typename T, int HD>
-__global__ __launch_bounds__(64 * kWaves, 2) void flash_alone_kernel(FlashArgs a) {
+__global__ __launch_bounds__(64 * kWaves, (Alone<T, HD>::WGS)) void flash_alone_kernel(FlashArgs a) {
   using O = Ops<T, HD>;
   using A = Alone<T, HD>;
   __shared__ __align__(16) typename A::Room lds;
@@ -653,8 +653,8 @@ struct DqRows {
 };
 
 // dQ, and what the pass over the keys needs, each (row, head) being one lane pair's.
-// The matrix pipe is busy 50% (heads of 128) and 65% (64) of the cycles: sixteen ragged rollouts
-// 392 to 420 us as the clock allows, one sequence of 8703 235.  Two waves a SIMD; tiles of 32
+// The matrix pipe is busy 51% (heads of 128) and 66% (64) of the cycles: sixteen ragged rollouts
+// 406 to 422 us as the clock allows, one sequence of 8703 236.  Two waves a SIMD; tiles of 32
 // keys, or four waves a SIMD of heads of 64, take the same time.
 template <typename T, int HD>
 __global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_dq_kernel(FlashArgs a) {
@@ -706,7 +706,7 @@ __global__ __launch_bounds__(64 * kWaves, (Ops<T, HD>::WGS)) void flash_dq_kerne
 }
 
 template <typename T, int HD>
-__global__ __launch_bounds__(64 * kWaves, 2) void flash_dq_alone_kernel(FlashArgs a) {
+__global__ __launch_bounds__(64 * kWaves, (Alone<T, HD>::WGS)) void flash_dq_alone_kernel(FlashArgs a) {
   using O = Ops<T, HD>;
   using A = Alone<T, HD>;
   __shared__ __align__(16) typename A::Room lds;
@@ -915,8 +915,8 @@ __device__ __forceinline__ void dk_step(f32x16_t* dk, const char* __restrict__ t
 //
 // The matrix pipe is busy 50% of the cycles; waves wait at the meetings and for LDS.  What bounds
 // a long run is power: the clock goes down to 1.7 GHz, and a form that took a quarter more
-// cycles ran at 1.9.  Sixteen ragged rollouts, 32 heads of 128 on 8: 585 us; one sequence of
-// 8703, 16 heads of 64 on 4: 352 to 363.  With float32 probabilities and both tiles a step longer, so two
+// cycles ran at 1.9.  Sixteen ragged rollouts, 32 heads of 128 on 8: 583 us; one sequence of
+// 8703, 16 heads of 64 on 4: 358.  With float32 probabilities and both tiles a step longer, so two
 // workgroups to a compute unit, 632 and 359; the second wave in the same step, at a second
 // meeting, 676 and 383; four pairs to a workgroup 645 (90 us for the backward pass of 200
 // sequences of at most 30, now 60), six 690.

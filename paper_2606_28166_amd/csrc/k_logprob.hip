@@ -188,7 +188,8 @@ __device__ __forceinline__ void fold(Stats& s, bool& far, const Eight<REF>& a, f
 }
 
 // A row (or its reference's) whose largest score the powers of two do not bear, or that has none
-// above -inf: in units of the logits, by one wave.
+// above -inf: in units of the logits, by one wave.  1024 rows of 151936 bf16 logits at T = 1e-7, all of them such,
+// 443 us and with a reference 676, where T = 1 takes 60 and 118.
 template <typename T, bool REF>
 __device__ __forceinline__ void logit_row(const LogprobArgs& a, int r, int lane) {
   const T* z = reinterpret_cast<const T*>(a.z) + (size_t)r * a.ldz;
@@ -285,7 +286,7 @@ __device__ __forceinline__ void left_out(const LogprobArgs& a, int r, bool ref) 
 // folds the last ones.
 //
 // Bound by HBM, with the vector unit close behind (13 operations for the 4
-// bytes of a bf16 logit and its reference): 2048 rows of 151936, a fifth left out, 208 us, 4.8 TB/s.
+// bytes of a bf16 logit and its reference): 2048 rows of 151936, a fifth left out, 201 us, 5.0 TB/s.
 template <typename T, bool REF, int NT>
 __global__ __launch_bounds__(256) void logprob_kernel(LogprobArgs a) {
   constexpr int RPB = 256 / NT;
@@ -362,7 +363,7 @@ __global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a) {
 }
 
 // Elementwise over kGradChunk entries of a row, bound by HBM: 1024 rows of 151936 bf16 logits
-// and their reference, a fifth left out, 155 us, 5.2 TB/s; 509 rows of 32001 float32 logits without
+// and their reference, a fifth left out, 151 us, 5.4 TB/s; 509 rows of 32001 float32 logits without
 // one 25 us, 4.6 TB/s.
 constexpr int kGradChunk = 8192;
 
@@ -437,7 +438,8 @@ __device__ __forceinline__ double workgroup_sum(double v, double* room) {
 
 // The same of other rows, and of those without a distribution: maximum, sum and mean difference
 // anew, in units of the logits, and from them dz_v = (g ([v = y] - p) + k p ((s_v - s'_v) - mean)) / T.
-// One workgroup takes the whole row: the gradient may take the logits' place.
+// One workgroup takes the whole row: the gradient may take the logits' place.  1024 rows of 151936
+// bf16 logits at T = 1e-3, all of them such, 539 us and with a reference 763, where T = 1 takes 115 and 177.
 template <typename T, bool KL>
 __device__ __forceinline__ void logit_grad(const LogprobArgs& a, float g, float k, const T* z, const T* zr, T* out,
                                            int y) {

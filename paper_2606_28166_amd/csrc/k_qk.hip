@@ -7,7 +7,7 @@
 // a lane belong to its position, so a lane keeps them over all the heads it takes
 // of one row.  An angle is turns = position * theta^(-2i/hd) / 2 pi in 64 bits, of
 // which the fraction is left: a far position loses nothing.  Memory bound: each
-// element once in, once out (backward: two in).  18432 rows of 40 heads of 128 take 72 us, 5.2 TB/s;
+// element once in, once out (backward: two in).  18432 rows of 40 heads of 128 take 71 us, 5.3 TB/s;
 // backward 4097 rows of 24 heads 21 us, 3.5 TB/s, and 4 for the gains' sums.
 //
 // The gains' gradients are summed in a lane over its rows, then over the
