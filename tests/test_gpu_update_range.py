@@ -188,3 +188,21 @@ def test_logprob_gradient_at_the_smallest_temperatures(dt):
             hot = torch.zeros((3, V), dtype=F64, device=z.device).scatter_(1, tok.long()[:, None], 1.0)
             want = gl.to(F64)[:, None] * (hot - 1.0 / V) * float(1.0 / torch.tensor(T, dtype=F32))
             _within(g, want, (_half(dt) + 64 * U) * want.abs(), "grad")
+
+
+@pytest.mark.parametrize("dt", [BF, F32], ids=["bf16", "f32"])
+def test_logprob_at_the_largest_temperatures(dt):
+    """1 / T is subnormal: every row is uniform, and no output is lost to it."""
+    from paper_2606_28166_amd import engine as E
+    for T in (1e38, 3.4e38):
+        for R, V in ((3, 50), (2, 40000), (1030, 2600)):
+            z, zr, tok, gl, gk = _inputs(R, V, dt, 1.0, -2.0, V)
+            f = E.token_logprob(z, tok, ref=zr, temperature=T)
+            one = torch.ones(R, dtype=F64, device=z.device)
+            _within(f["logp"], -math.log(V) * one, 16 * U * math.log(V) * one, "logp")
+            _within(f["lse"], math.log(V) * one, 16 * U * math.log(V) * one, "lse")
+            for name in ("kl", "lse_diff"):
+                _within(f[name], 0 * one, 32 * U * one, name)
+            g = E.token_logprob_backward(z, tok, f, gl, g_kl=gk, ref=zr, temperature=T)
+            # at most |g| / T, which is about the smallest normal number
+            assert torch.isfinite(g).all() and float(g.float().abs().max()) <= 4 * 2.0 ** -126
