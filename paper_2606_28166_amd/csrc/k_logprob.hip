@@ -169,11 +169,22 @@ __device__ __forceinline__ void fold(Stats& s, bool& far, const Eight<REF>& a, f
     s.lr += (double)lr;
     // scores of -inf on either side: an entry of probability 0 adds nothing, whatever they differ by
     if (__any(far || lo == -INFINITY)) {
+      if (__any(far)) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          s.l += (double)p[e];
+          s.w += p[e] > 0.f ? (double)p[e] * ((double)a.x[e] - (double)a.y[e]) : (double)p[e];
+        }
+        return;
+      }
+      float l = 0.f, w = 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        s.l += (double)p[e];
-        s.w += p[e] > 0.f ? (double)p[e] * ((double)a.x[e] - (double)a.y[e]) : (double)p[e];
+        l += p[e];
+        w += p[e] > 0.f ? p[e] * (a.x[e] - a.y[e]) : p[e];
       }
+      s.l += (double)l;
+      s.w += (double)w;
       return;
     }
   }
