@@ -379,8 +379,8 @@ __global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a) {
 constexpr int kGradChunk = 8192;
 
 // Up to what log-sum-exp, and mean difference of the two models' scores, a row's gradient takes
-// them as they were rounded: half a step of lse is an error of p, here an eighth of the
-// result's own rounding in bf16, 2^-17 in float32.
+// them as they were rounded: half a step of lse is an error of p, in bf16 2^-13, a 32nd of the
+// result's own rounding, in float32 2^-17.
 template <typename T> constexpr float kGradMost = sizeof(T) == 2 ? 4096.f : 256.f;
 
 // What a row's gradient is made of: dz_v = p (A + B (z_v - z'_v)), and `at` more at the token.

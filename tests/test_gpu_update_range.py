@@ -108,9 +108,9 @@ def test_logprob_of_large_rows_beside_masked_entries(dt):
                 assert ((r[n] - ref[n]).abs() <= 32 * U * size).all(), (n, V, a, b)
 
 
-# The gradient takes p = e^(s - lse) from the float32 lse, which is off by u |lse|, up to a log-sum-exp (and a
-# mean difference of the models' scores) of this much: an eighth of half a step of bf16, 2^-16 in float32.  Other
-# rows are summed anew.
+# The gradient takes p = e^(s - lse) from the float32 lse, which is off by at most u |lse|, up to a log-sum-exp (and a
+# mean difference of the models' scores) of this much: 2^-12 in bf16, a sixteenth of half a step, 2^-16 in float32.
+# Other rows are summed anew.
 GRAD_LIMIT = {BF: 4096.0, F32: 256.0}
 
 
